@@ -324,6 +324,101 @@ int kvq_unpack_codes(const kvq_cache_desc* desc, int which, int64_t begin, int64
 int kvq_status_word_result(int32_t status_word_value);
 int kvq_set_wait_budget_cycles(uint64_t cycles);
 
+/* ---- paged 8-bit cache ----------------------------------------------------------------------------------------
+ *
+ * The near-lossless form beside the low-bit cache above, for requests of different lengths: keys and values as E4M3 codes
+ * in pages of a pool, one scale for each page and head.  Causal masks, sliding windows, key heads shared by groups of query
+ * heads, and the rotation of queries and keys by their positions belong to it; the Hadamard rotation and the bias correction
+ * do not (an E4M3 step depends on the number, so the correction's model of uniform noise does not hold, and at 8 bits the bias
+ * it removes is far below the rounding of the output).
+ *
+ *   codes  u8 [pages, kv_heads, page, head_dim]   E4M3
+ *   scale  u8 [pages, kv_heads]                   a byte s stands for 2^(s - 127); a number is code * scale
+ *
+ * A power of two, because E4M3's relative precision does not depend on its scale: a page whose scale grows with later tokens is
+ * moved to the new one without a second rounding of any code in the format's normal range.
+ * All four buffers must be zeroed once before their first use (slots that no token fills take part in products, with weight
+ * zero); pages can be given to other sequences without clearing.
+ */
+typedef struct kvq_paged_cache {     /* one layer's pool; host memory */
+  int32_t  kv_heads, head_dim;       /* head_dim: 64 or 128 */
+  int32_t  page;                     /* tokens per page: 16, 32, 64 or 128 */
+  uint32_t flags;                    /* 0 */
+  int64_t  pages;
+  void*    k_codes;  void* v_codes;  /* device, 16-byte aligned */
+  void*    k_scale;  void* v_scale;  /* device */
+} kvq_paged_cache;
+
+/* The sequences of a call; shared by all layers of a step.  Token j of sequence b lies in slot j % page of page
+ * page_table[b * table_stride + j / page].  Entries beyond a sequence's tokens are not read. */
+typedef struct kvq_paged_batch {
+  int32_t batch, table_width;        /* sequences; entries of a table row; table_width * page < 2^31 - 128 */
+  int64_t table_stride;              /* entries from one row to the next */
+  const int32_t* page_table;         /* device */
+  const int32_t* lengths;            /* device [batch]: tokens before the call's new ones */
+  const int32_t* n_new;              /* device [batch]: new tokens, of the call's n_tokens / m_tokens; NULL: all of them */
+} kvq_paged_batch;
+
+/* Position rotation of the first `dim` channels of keys and queries: the pair (x, y) of index i becomes
+ * (x cos - y sin, y cos + x sin) with cos, sin = row (position), column i of the tables.  Channels i and i + dim / 2 are a pair, or
+ * 2 i and 2 i + 1 with KVQ_ROPE_INTERLEAVED.  All in binary32, every product and sum rounded by itself. */
+#define KVQ_ROPE_INTERLEAVED  1u
+typedef struct kvq_rope {
+  const float* cos;  const float* sin;   /* device [rows, dim / 2], 16-byte aligned */
+  const int32_t* positions;              /* device: row of new token t of sequence b at [b * positions_stride + t]; NULL: lengths[b] + t */
+  int64_t  positions_stride;
+  int32_t  rows, dim;                    /* dim: a multiple of 16, at most head_dim; 0: no rotation */
+  uint32_t flags;
+} kvq_rope;
+
+/* What these calls leave in their status word (optional device int32, zero on entry; the first one is kept).  The call has done what it
+ * could, and touched nothing out of bounds: 501 a page number that the pool does not have (its tokens are not written, not seen), 502 a
+ * position that the tables do not have (the nearest row stands for it), 503 lengths that are negative or longer than the table row
+ * (what it cannot hold is left out). */
+#define KVQ_PAGED_BAD_PAGE      501
+#define KVQ_PAGED_BAD_POSITION  502
+#define KVQ_PAGED_BAD_LENGTH    503
+
+/* Sizes in bytes of k_codes, v_codes, k_scale, v_scale.  Errors: KVQ_ERR_INVALID_ARG, KVQ_ERR_UNSUPPORTED. */
+int kvq_paged_cache_bytes(const kvq_paged_cache* cache, size_t out_bytes[4]);
+
+/*
+ * Appends new tokens: tokens [0, n_new[b]) of k, v (device BF16 [batch, kv_heads, n_tokens, head_dim], strides of their own) become
+ * tokens lengths[b] ... of sequence b.  Per block (the tokens of one page and head):
+ *   y    = rotated keys, values as they are
+ *   e    = the smallest exponent with max |y| <= 448 * 2^e over the block's new tokens, at least -64; a page that holds earlier
+ *          tokens keeps its exponent if that is larger, and otherwise its codes move to the new one
+ *   code = E4M3(y * 2^-e), nearest even
+ * Infinities do not count for the maximum and saturate at 448.  A NaN in a token's keys or values makes all of its key codes of that head NaN and
+ * its NaN values 0: queries that see the token answer NaN, others do not.
+ * A page that is written by this call must belong to one sequence only.  lengths is not changed.
+ * Errors: KVQ_ERR_INVALID_ARG, KVQ_ERR_UNSUPPORTED, KVQ_ERR_ALIGNMENT, KVQ_ERR_CUDA.  n_tokens == 0 and batch == 0 are no-ops.
+ */
+int kvq_paged_append(const kvq_paged_cache* cache, const kvq_paged_batch* seqs, const kvq_rope* rope,
+                     const void* k_bf16, kvq_strides k_strides, const void* v_bf16, kvq_strides v_strides,
+                     int64_t n_tokens, int32_t* status_word, kvq_stream_t stream);
+
+/*
+ * Attention of the sequences' new tokens over their pages, which hold those tokens too (kvq_paged_append comes first).  Query t < n_new[b] of
+ * head h of sequence b stands at position i = lengths[b] + t and sees, of the lengths[b] + n_new[b] tokens,
+ *   KVQ_PAGED_CAUSAL    those with j <= i; with window > 0 of these the last `window`, j > i - window
+ *   0                   all (window must be 0)
+ *   s_j = softmax_scale * rope(q) . k_j,  out = sum_j exp(s_j) v_j / sum_j exp(s_j)      over key head h / (q_heads / kv_heads)
+ * A query that sees no key, and rows t >= n_new[b], give 0 (and a log-sum-exp of -infinity).
+ * q, out: device BF16 [batch, q_heads, m_tokens, head_dim], strides of their own.  lse_out: optional device float
+ * [batch, q_heads, m_tokens], natural log of the denominator.  workspace: as for kvq_attn_corrected, of at least
+ * kvq_paged_attn_workspace_bytes() bytes, 256-byte aligned, contents need not be initialised.
+ * Errors: KVQ_ERR_INVALID_ARG, KVQ_ERR_UNSUPPORTED, KVQ_ERR_ALIGNMENT, KVQ_ERR_WORKSPACE, KVQ_ERR_CUDA.  m_tokens == 0 and batch == 0
+ * are no-ops.
+ */
+#define KVQ_PAGED_CAUSAL  1u
+int kvq_paged_attn(const kvq_paged_cache* cache, const kvq_paged_batch* seqs, const kvq_rope* rope,
+                   const void* q_bf16, kvq_strides q_strides, int32_t q_heads, int64_t m_tokens,
+                   void* out_bf16, kvq_strides o_strides, float softmax_scale, int64_t window, uint32_t flags,
+                   float* lse_out, void* workspace, size_t workspace_bytes, int32_t* status_word, kvq_stream_t stream);
+int kvq_paged_attn_workspace_bytes(const kvq_paged_cache* cache, const kvq_paged_batch* seqs, int32_t q_heads,
+                                   int64_t m_tokens, uint32_t flags, size_t* out_bytes);
+
 /* Host-side helpers. */
 const char* kvq_status_string(int status);   /* static string, never NULL */
 int kvq_last_cuda_error(void);               /* cudaError_t of the last KVQ_ERR_CUDA on this thread, else 0 */

@@ -26,6 +26,8 @@ KVQ_RING = 2
 KVQ_ROTATE_V = 4
 KVQ_K_PER_CHANNEL = 8
 KVQ_CORRECTION_OFF, KVQ_CORRECTION_ON, KVQ_CORRECTION_EXACT = 0, 1, 2
+KVQ_ROPE_INTERLEAVED, KVQ_PAGED_CAUSAL = 1, 1
+KVQ_PAGED_BAD_PAGE, KVQ_PAGED_BAD_POSITION, KVQ_PAGED_BAD_LENGTH = 501, 502, 503
 KVQ_KERNEL_AUTO, KVQ_KERNEL_MMA_SYNC, KVQ_KERNEL_TCGEN05, KVQ_KERNEL_TCGEN05_PAIR = 0, 1 << 8, 2 << 8, 3 << 8
 
 
@@ -43,6 +45,21 @@ class kvq_cache_desc(C.Structure):
 
 class kvq_strides(C.Structure):
     _fields_ = [("b", C.c_int64), ("h", C.c_int64), ("t", C.c_int64)]
+
+
+class kvq_paged_cache(C.Structure):
+    _fields_ = [("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page", C.c_int32), ("flags", C.c_uint32), ("pages", C.c_int64),
+                ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class kvq_paged_batch(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("table_width", C.c_int32), ("table_stride", C.c_int64),
+                ("page_table", C.c_void_p), ("lengths", C.c_void_p), ("n_new", C.c_void_p)]
+
+
+class kvq_rope(C.Structure):
+    _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p), ("positions", C.c_void_p), ("positions_stride", C.c_int64),
+                ("rows", C.c_int32), ("dim", C.c_int32), ("flags", C.c_uint32)]
 
 
 def _load():
@@ -89,6 +106,19 @@ def _load():
     lib.kvq_unpack_codes.restype = C.c_int
     lib.kvq_unpack_codes.argtypes = [C.POINTER(kvq_cache_desc), C.c_int, C.c_int64, C.c_int64,
                                      C.c_void_p, C.c_void_p]
+    P = C.POINTER
+    lib.kvq_paged_cache_bytes.restype = C.c_int
+    lib.kvq_paged_cache_bytes.argtypes = [P(kvq_paged_cache), P(C.c_size_t)]
+    lib.kvq_paged_append.restype = C.c_int
+    lib.kvq_paged_append.argtypes = [P(kvq_paged_cache), P(kvq_paged_batch), P(kvq_rope), C.c_void_p, kvq_strides, C.c_void_p,
+                                     kvq_strides, C.c_int64, C.c_void_p, C.c_void_p]
+    lib.kvq_paged_attn.restype = C.c_int
+    lib.kvq_paged_attn.argtypes = [P(kvq_paged_cache), P(kvq_paged_batch), P(kvq_rope), C.c_void_p, kvq_strides, C.c_int32,
+                                   C.c_int64, C.c_void_p, kvq_strides, C.c_float, C.c_int64, C.c_uint32, C.c_void_p, C.c_void_p,
+                                   C.c_size_t, C.c_void_p, C.c_void_p]
+    lib.kvq_paged_attn_workspace_bytes.restype = C.c_int
+    lib.kvq_paged_attn_workspace_bytes.argtypes = [P(kvq_paged_cache), P(kvq_paged_batch), C.c_int32, C.c_int64, C.c_uint32,
+                                                   P(C.c_size_t)]
     return lib
 
 
@@ -353,4 +383,124 @@ def kvq_unpack_codes(cache: Cache, which: int, begin: int, n: int) -> torch.Tens
     d = cache.desc
     out = torch.empty((d.batch, d.heads, n, d.head_dim), dtype=torch.uint8, device=cache.buffers[0].device)
     _check(lib.kvq_unpack_codes(C.byref(d), which, begin, n, out.data_ptr(), _stream()), "kvq_unpack_codes")
+    return out
+
+
+# ---- paged 8-bit cache --------------------------------------------------------------------------
+
+
+class PagedCache:
+    """Caller-side owner of one layer's pool of pages: E4M3 codes [pages, kv_heads, page, head_dim] and scale bytes
+    [pages, kv_heads], of keys and of values.  `buffers` (k_codes, v_codes, k_scale, v_scale) adopts a pool that exists; the
+    buffers of a new one are zeros, as the kernels want them before their first use."""
+
+    def __init__(self, pages, kv_heads, head_dim, page=64, device="cuda", buffers=None):
+        self.desc = kvq_paged_cache(kv_heads, head_dim, page, 0, pages)
+        sizes = kvq_paged_cache_bytes(self.desc)
+        if buffers is None:
+            buffers = [torch.zeros(n, dtype=torch.uint8, device=device) for n in sizes]
+        assert len(buffers) == 4 and all(b.is_contiguous() and b.element_size() == 1 and b.numel() == n
+                                         for b, n in zip(buffers, sizes)), "four contiguous buffers of one byte an element"
+        self.buffers = list(buffers)
+        self.desc.k_codes, self.desc.v_codes, self.desc.k_scale, self.desc.v_scale = [b.data_ptr() for b in self.buffers]
+        self._workspaces = {}
+
+    def views(self):
+        """The four buffers shaped [pages, kv_heads, ...]: codes as float8_e4m3fn, scales as bytes (2^(byte - 127))."""
+        d = self.desc
+        kc, vc, ks, vs = (b.view(torch.uint8) for b in self.buffers)
+        codes = (d.pages, d.kv_heads, d.page, d.head_dim)
+        return {"k_codes": kc.view(codes).view(torch.float8_e4m3fn), "v_codes": vc.view(codes).view(torch.float8_e4m3fn),
+                "k_scale": ks.view(d.pages, d.kv_heads), "v_scale": vs.view(d.pages, d.kv_heads)}
+
+    def _workspace(self, need, stream, device):
+        """A buffer for each stream (at most eight are kept), a fresh one for a call that is being captured."""
+        capturing = _capturing()
+        ws = None if capturing else self._workspaces.get(stream)
+        if ws is None or ws.numel() < need:
+            ws = torch.empty(need, dtype=torch.uint8, device=device)
+            if not capturing:
+                if stream not in self._workspaces and len(self._workspaces) >= 8:
+                    self._workspaces.pop(list(self._workspaces)[0], None)
+                self._workspaces[stream] = ws
+        return ws
+
+
+def kvq_paged_cache_bytes(desc: kvq_paged_cache):
+    out = (C.c_size_t * 4)()
+    _check(lib.kvq_paged_cache_bytes(C.byref(desc), out), "kvq_paged_cache_bytes")
+    return list(out)
+
+
+def _paged_strides(t, heads, head_dim):
+    """Strides of a BF16 tensor [batch, heads, tokens, head_dim]; those of a dimension of one element do not matter and are made plain."""
+    assert t.dtype is _BF16 and t.is_cuda and t.dim() == 4 and t.shape[1] == heads and t.shape[3] == head_dim
+    sb, sh, st, sd = t.stride()
+    assert sd == 1, "tensor must be [batch, heads, tokens, head_dim] with unit inner stride"
+    n = t.shape
+    return kvq_strides(sb if n[0] > 1 else 0, sh if n[1] > 1 else 0, st if n[2] > 1 else head_dim)
+
+
+def _paged_batch(batch, n, page_table, lengths, n_new):
+    for t in (page_table, lengths) if n_new is None else (page_table, lengths, n_new):
+        assert t.dtype is torch.int32 and t.is_cuda
+    assert page_table.dim() == 2 and page_table.shape[0] == batch and (page_table.shape[1] < 2 or page_table.stride(1) == 1)
+    assert lengths.shape == (batch,) and lengths.is_contiguous()
+    assert n_new is None or (n_new.shape == (batch,) and n_new.is_contiguous())
+    width = page_table.shape[1]
+    return kvq_paged_batch(batch, width, page_table.stride(0) if batch > 1 else width, page_table.data_ptr(), lengths.data_ptr(), _ptr(n_new))
+
+
+def _paged_rope(batch, n, cos, sin, positions, interleaved):
+    if cos is None:
+        assert sin is None and positions is None
+        return None
+    for t in (cos, sin):
+        assert t.dtype is torch.float32 and t.is_cuda and t.dim() == 2 and t.is_contiguous()
+    assert cos.shape == sin.shape
+    if positions is not None:
+        assert positions.dtype is torch.int32 and positions.is_cuda and positions.shape == (batch, n)
+        assert n < 2 or positions.stride(1) == 1
+    return C.byref(kvq_rope(cos.data_ptr(), sin.data_ptr(), _ptr(positions), positions.stride(0) if positions is not None and batch > 1 else n,
+                            cos.shape[0], 2 * cos.shape[1], KVQ_ROPE_INTERLEAVED if interleaved else 0))
+
+
+def kvq_paged_append(cache: PagedCache, k, v, page_table, lengths, n_new=None, cos=None, sin=None, positions=None,
+                     interleaved=False, status_word=None):
+    """Writes new tokens k, v ([batch, kv_heads, n, head_dim] BF16, CUDA; n_new[b] of them are real) behind the `lengths` (int32
+    [batch]) tokens that the sequences of `page_table` (int32 [batch, width]) hold.  cos, sin: float32 [rows, dim / 2], rotate the
+    keys; positions: int32 [batch, n], the tables' rows of the tokens (default: their places in the sequence)."""
+    batch, n = k.shape[0], k.shape[2]
+    assert k.shape == v.shape
+    d = cache.desc
+    _check(lib.kvq_paged_append(
+        C.byref(d), C.byref(_paged_batch(batch, n, page_table, lengths, n_new)), _paged_rope(batch, n, cos, sin, positions, interleaved),
+        k.data_ptr(), _paged_strides(k, d.kv_heads, d.head_dim), v.data_ptr(), _paged_strides(v, d.kv_heads, d.head_dim), n, _ptr(status_word), _stream()),
+        "kvq_paged_append")
+
+
+def kvq_paged_attn_workspace_bytes(cache: PagedCache, batch: kvq_paged_batch, q_heads: int, m_tokens: int, flags: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib.kvq_paged_attn_workspace_bytes(C.byref(cache.desc), C.byref(batch), q_heads, m_tokens, flags, C.byref(out)),
+           "kvq_paged_attn_workspace_bytes")
+    return out.value
+
+
+def kvq_paged_attn(cache: PagedCache, q, page_table, lengths, softmax_scale, n_new=None, causal=True, window=0, cos=None, sin=None,
+                   positions=None, interleaved=False, out=None, lse=None, status_word=None):
+    """Attention of the new tokens q ([batch, q_heads, m, head_dim] BF16, CUDA) over the tokens of their sequences, which have
+    been appended; page_table, lengths, n_new, cos, sin, positions as for the append.  Returns `out` (allocated if not given)."""
+    batch, heads, m, head_dim = q.shape
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    assert out.shape == q.shape
+    if lse is not None:
+        assert lse.dtype is torch.float32 and lse.is_cuda and lse.is_contiguous() and lse.shape == q.shape[:3]
+    seqs, flags, stream = _paged_batch(batch, m, page_table, lengths, n_new), KVQ_PAGED_CAUSAL if causal else 0, _stream()
+    need = kvq_paged_attn_workspace_bytes(cache, seqs, heads, m, flags)
+    ws = cache._workspace(need, stream, q.device) if need else None
+    _check(lib.kvq_paged_attn(
+        C.byref(cache.desc), C.byref(seqs), _paged_rope(batch, m, cos, sin, positions, interleaved), q.data_ptr(),
+        _paged_strides(q, heads, cache.desc.head_dim), heads, m, out.data_ptr(), _paged_strides(out, heads, cache.desc.head_dim),
+        float(softmax_scale), int(window), flags, _ptr(lse), _ptr(ws), need, _ptr(status_word), stream), "kvq_paged_attn")
     return out

@@ -14,7 +14,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libkvq.so")
-SOURCES = ["kvq_api.cu", "quantize_append.cu", "rotate_rows.cu", "attn_mma_sync.cu", "attn_jsd.cu", "attn_short.cu", "attn_sm100.cu"]
+SOURCES = ["kvq_api.cu", "quantize_append.cu", "rotate_rows.cu", "attn_mma_sync.cu", "attn_jsd.cu", "attn_short.cu", "attn_sm100.cu",
+           "paged/api.cu", "paged/append.cu", "paged/attn.cu"]
 HEADERS = [os.path.join(CSRC, "kvq_common.cuh"), os.path.join(ROOT, "include", "kvq.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -73,7 +74,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
 
 
 def _build_locked(force: bool, verbose: bool) -> str:
-    headers = sorted(set(HEADERS + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]))
+    headers = sorted(set(HEADERS + [os.path.join(d, f) for d in (CSRC, os.path.join(CSRC, "paged")) for f in os.listdir(d) if f.endswith((".cuh", ".h"))]))
 
     def compile_one(src: str):
         s = os.path.join(CSRC, src)

@@ -1,0 +1,139 @@
+// C-ABI entry points of the paged 8-bit cache: argument checks, then the launchers.
+#include "paged.cuh"
+
+namespace kvq {
+namespace paged {
+namespace {
+
+int check_cache(const kvq_paged_cache* c, bool pointers) {
+  if (!c) return KVQ_ERR_INVALID_ARG;
+  if (c->kv_heads <= 0 || c->head_dim <= 0 || c->page <= 0 || c->pages <= 0 || c->flags) return KVQ_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return KVQ_ERR_UNSUPPORTED;
+  if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return KVQ_ERR_UNSUPPORTED;
+  if (c->kv_heads > 65535 || c->pages > 0x7FFFFFFFLL) return KVQ_ERR_UNSUPPORTED;
+  if (!pointers) return KVQ_OK;
+  const void* codes[2] = {c->k_codes, c->v_codes};
+  for (const void* p : codes) {
+    if (!p) return KVQ_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return KVQ_ERR_ALIGNMENT;
+  }
+  if (!c->k_scale || !c->v_scale) return KVQ_ERR_INVALID_ARG;
+  return KVQ_OK;
+}
+
+int check_batch(const kvq_paged_cache* c, const kvq_paged_batch* s, bool pointers) {
+  if (!s) return KVQ_ERR_INVALID_ARG;
+  if (s->batch < 0 || s->table_width < 0 || s->table_stride < 0) return KVQ_ERR_INVALID_ARG;
+  if (s->batch > 1 && s->table_stride < s->table_width) return KVQ_ERR_INVALID_ARG;
+  if (s->batch > 65535 || (int64_t)s->table_width * c->page > 0x7FFFFFFFLL - 128) return KVQ_ERR_UNSUPPORTED;
+  if (!pointers || s->batch == 0) return KVQ_OK;
+  if (!s->lengths || (s->table_width > 0 && !s->page_table)) return KVQ_ERR_INVALID_ARG;
+  const void* ints[3] = {s->page_table, s->lengths, s->n_new};
+  for (const void* p : ints)
+    if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return KVQ_ERR_ALIGNMENT;
+  return KVQ_OK;
+}
+
+int check_rope(const kvq_paged_cache* c, const kvq_rope* r, Rope* out) {
+  *out = Rope{};
+  if (!r || r->dim == 0) return KVQ_OK;
+  if (r->dim < 0 || r->dim > c->head_dim || r->rows <= 0 || r->positions_stride < 0 || !r->cos || !r->sin) return KVQ_ERR_INVALID_ARG;
+  if (r->flags & ~KVQ_ROPE_INTERLEAVED) return KVQ_ERR_INVALID_ARG;
+  if (r->dim % 16 != 0) return KVQ_ERR_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(r->cos) % 16 != 0 || reinterpret_cast<uintptr_t>(r->sin) % 16 != 0 ||
+      reinterpret_cast<uintptr_t>(r->positions) % 4 != 0)
+    return KVQ_ERR_ALIGNMENT;
+  *out = Rope{r->cos, r->sin, r->positions, r->positions_stride, r->rows, r->dim, (r->flags & KVQ_ROPE_INTERLEAVED) != 0};
+  return KVQ_OK;
+}
+
+Pool pool_of(const kvq_paged_cache* c) {
+  int log2_page = 0;
+  while ((1 << log2_page) < c->page) ++log2_page;
+  return Pool{static_cast<uint8_t*>(c->k_codes), static_cast<uint8_t*>(c->v_codes), static_cast<uint8_t*>(c->k_scale),
+              static_cast<uint8_t*>(c->v_scale), c->kv_heads, c->page, log2_page, c->pages};
+}
+
+Seqs seqs_of(const kvq_paged_batch* s) { return Seqs{s->page_table, s->lengths, s->n_new, s->table_stride, s->batch, s->table_width}; }
+
+int check_attn_sizes(const kvq_paged_cache* c, const kvq_paged_batch* s, int32_t q_heads, int64_t m_tokens, uint32_t flags, bool pointers) {
+  int r = check_cache(c, pointers);
+  if (r != KVQ_OK) return r;
+  if ((r = check_batch(c, s, pointers)) != KVQ_OK) return r;
+  if (q_heads <= 0 || q_heads % c->kv_heads != 0 || m_tokens < 0) return KVQ_ERR_INVALID_ARG;
+  if (flags & ~KVQ_PAGED_CAUSAL) return KVQ_ERR_INVALID_ARG;
+  if (q_heads > 65535 || m_tokens > 0x7FFFFFFFLL / q_heads) return KVQ_ERR_UNSUPPORTED;
+  return KVQ_OK;
+}
+
+}  // namespace
+}  // namespace paged
+}  // namespace kvq
+
+using namespace kvq;
+using namespace kvq::paged;
+
+extern "C" {
+
+int kvq_paged_cache_bytes(const kvq_paged_cache* cache, size_t out_bytes[4]) {
+  const int r = check_cache(cache, false);
+  if (r != KVQ_OK) return r;
+  if (!out_bytes) return KVQ_ERR_INVALID_ARG;
+  const size_t blocks = (size_t)cache->pages * cache->kv_heads;
+  out_bytes[0] = out_bytes[1] = blocks * cache->page * cache->head_dim;
+  out_bytes[2] = out_bytes[3] = blocks;
+  return KVQ_OK;
+}
+
+int kvq_paged_append(const kvq_paged_cache* cache, const kvq_paged_batch* seqs, const kvq_rope* rope, const void* k_bf16,
+                     kvq_strides k_strides, const void* v_bf16, kvq_strides v_strides, int64_t n_tokens, int32_t* status_word,
+                     kvq_stream_t stream) {
+  int r = check_cache(cache, true);
+  if (r != KVQ_OK) return r;
+  if ((r = check_batch(cache, seqs, true)) != KVQ_OK) return r;
+  if (n_tokens < 0) return KVQ_ERR_INVALID_ARG;
+  if (n_tokens > 0x7FFFFFFFLL - 256) return KVQ_ERR_UNSUPPORTED;
+  AppendCall c;
+  if ((r = check_rope(cache, rope, &c.rope)) != KVQ_OK) return r;
+  if (n_tokens == 0 || seqs->batch == 0) return KVQ_OK;
+  if ((r = check_tensor(k_bf16, k_strides)) != KVQ_OK) return r;
+  if ((r = check_tensor(v_bf16, v_strides)) != KVQ_OK) return r;
+  c.pool = pool_of(cache); c.seqs = seqs_of(seqs); c.head_dim = cache->head_dim;
+  c.k = k_bf16; c.v = v_bf16; c.ks = k_strides; c.vs = v_strides; c.n_tokens = n_tokens;
+  c.status = status_word; c.stream = (cudaStream_t)stream;
+  return launch_append(c);
+}
+
+int kvq_paged_attn_workspace_bytes(const kvq_paged_cache* cache, const kvq_paged_batch* seqs, int32_t q_heads, int64_t m_tokens,
+                                   uint32_t flags, size_t* out_bytes) {
+  const int r = check_attn_sizes(cache, seqs, q_heads, m_tokens, flags, false);
+  if (r != KVQ_OK) return r;
+  if (!out_bytes) return KVQ_ERR_INVALID_ARG;
+  *out_bytes = 0;
+  return KVQ_OK;
+}
+
+int kvq_paged_attn(const kvq_paged_cache* cache, const kvq_paged_batch* seqs, const kvq_rope* rope, const void* q_bf16,
+                   kvq_strides q_strides, int32_t q_heads, int64_t m_tokens, void* out_bf16, kvq_strides o_strides,
+                   float softmax_scale, int64_t window, uint32_t flags, float* lse_out, void* workspace, size_t workspace_bytes,
+                   int32_t* status_word, kvq_stream_t stream) {
+  int r = check_attn_sizes(cache, seqs, q_heads, m_tokens, flags, true);
+  if (r != KVQ_OK) return r;
+  if (window < 0 || (window > 0 && !(flags & KVQ_PAGED_CAUSAL))) return KVQ_ERR_INVALID_ARG;
+  if (!(softmax_scale > 0.0f) || !(softmax_scale < 1e30f)) return KVQ_ERR_INVALID_ARG;
+  AttnCall c;
+  if ((r = check_rope(cache, rope, &c.rope)) != KVQ_OK) return r;
+  if (m_tokens == 0 || seqs->batch == 0) return KVQ_OK;
+  if ((r = check_tensor(q_bf16, q_strides)) != KVQ_OK) return r;
+  if ((r = check_tensor(out_bf16, o_strides)) != KVQ_OK) return r;
+  c.pool = pool_of(cache); c.seqs = seqs_of(seqs); c.head_dim = cache->head_dim;
+  c.q_heads = q_heads; c.group = q_heads / cache->kv_heads;
+  c.q = q_bf16; c.qs = q_strides; c.out = out_bf16; c.os = o_strides; c.m_tokens = m_tokens;
+  c.softmax_scale = softmax_scale; c.causal = (flags & KVQ_PAGED_CAUSAL) != 0;
+  c.window = window > 0x7FFFFFFFLL ? 0 : window;             // no sequence is longer
+  c.lse = lse_out; c.workspace = workspace; c.workspace_bytes = workspace_bytes; c.status = status_word;
+  c.stream = (cudaStream_t)stream;
+  return launch_attn(c);
+}
+
+}  // extern "C"

@@ -1,0 +1,161 @@
+// Shared by the kernels of the paged 8-bit cache (internal; not part of the C ABI).
+#pragma once
+#include "kvq_common.cuh"
+
+namespace kvq {
+namespace paged {
+
+// Diagnostics that a kernel leaves in the caller's status word (kvq.h).
+constexpr int kBadPage = 501, kBadPosition = 502, kBadLength = 503;
+
+constexpr int kExpBias = 127;      // a scale byte b stands for 2^(b - 127)
+constexpr int kExpMin = -64;       // the smallest exponent an append gives a block
+
+// The pool, the sequences and the rotation of a call, as the kernels take them.
+struct Pool {
+  uint8_t *k_codes, *v_codes, *k_scale, *v_scale;
+  int kv_heads, page, log2_page;
+  int64_t pages;
+};
+struct Seqs {
+  const int32_t *table, *lengths, *n_new;
+  int64_t table_stride;
+  int batch, width;
+};
+struct Rope {
+  const float *cos, *sin;
+  const int32_t* positions;
+  int64_t positions_stride;
+  int rows, dim;                   // dim 0: no rotation
+  bool interleaved;
+};
+
+struct AttnCall {
+  Pool pool;
+  Seqs seqs;
+  Rope rope;
+  int head_dim, q_heads, group;    // group: query heads of a key head
+  const void* q; kvq_strides qs;
+  void* out; kvq_strides os;
+  int64_t m_tokens;
+  float softmax_scale;
+  bool causal;
+  int64_t window;                  // 0: none
+  float* lse;
+  void* workspace; size_t workspace_bytes;
+  int32_t* status;
+  cudaStream_t stream;
+};
+
+struct AppendCall {
+  Pool pool;
+  Seqs seqs;
+  Rope rope;
+  int head_dim;
+  const void *k, *v; kvq_strides ks, vs;
+  int64_t n_tokens;
+  int32_t* status;
+  cudaStream_t stream;
+};
+
+int launch_append(const AppendCall& c);
+int launch_attn(const AttnCall& c);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void report(int32_t* status, int code) {
+  if (status) atomicCAS(status, 0, code);
+}
+
+// Tokens of a sequence before the call's new ones, and the new ones that are real.  What the table cannot hold is left out.
+struct Extent { int before, fresh; };
+__device__ __forceinline__ Extent extent_of(const Seqs& s, int page, int b, int64_t n_tokens, int32_t* status) {
+  const int64_t room = (int64_t)s.width * page;
+  int64_t before = load_coherent(s.lengths + b);
+  int64_t fresh = s.n_new ? (int64_t)load_coherent(s.n_new + b) : n_tokens;
+  fresh = fresh < 0 ? 0 : fresh > n_tokens ? n_tokens : fresh;
+  const bool bad = before < 0 || before + fresh > room;
+  if (before < 0) before = 0;
+  if (before > room) before = room;
+  if (before + fresh > room) fresh = room - before;
+  if (bad) report(status, kBadLength);
+  return {(int)before, (int)fresh};
+}
+
+// Row of the rotation's tables for new token t of sequence b.
+__device__ __forceinline__ int rope_row(const Rope& r, int b, int t, int before, int32_t* status) {
+  int row = r.positions ? load_coherent(r.positions + (int64_t)b * r.positions_stride + t) : before + t;
+  if (row < 0 || row >= r.rows) {
+    report(status, kBadPosition);
+    row = row < 0 ? 0 : r.rows - 1;
+  }
+  return row;
+}
+
+// Rotates the 8 channels [8 j, 8 j + 8) that this lane holds of a row of D channels spread over D / 8 neighbouring lanes (all of
+// them here).  cs, sn: the row of the tables.  Every product and sum is rounded by itself, so that the result is that of the
+// formulas in binary32, whoever computes them.  Pairs lie side by side (interleaved), or dim / 2 channels apart, in another lane.
+__device__ __forceinline__ void rotate8(float (&x)[8], const float* cs, const float* sn, const Rope& r, int j) {
+  const int chunks = r.dim >> 3;
+  if (r.interleaved) {
+    if (j < chunks) {
+      const float4 c = *reinterpret_cast<const float4*>(cs + 4 * j), s = *reinterpret_cast<const float4*>(sn + 4 * j);
+      const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float a = x[2 * i], b = x[2 * i + 1];
+        x[2 * i] = __fsub_rn(__fmul_rn(a, cc[i]), __fmul_rn(b, ss[i]));
+        x[2 * i + 1] = __fadd_rn(__fmul_rn(b, cc[i]), __fmul_rn(a, ss[i]));
+      }
+    }
+    return;
+  }
+  const int half = chunks >> 1;
+  const int lane = threadIdx.x & 31;
+  const bool low = j < half, in = j < chunks;
+  const int from = in ? (low ? lane + half : lane - half) : lane;
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xFFFFFFFFu, x[i], from);
+  if (in) {
+    const int at = 8 * (low ? j : j - half);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 c = *reinterpret_cast<const float4*>(cs + at + 4 * h), s = *reinterpret_cast<const float4*>(sn + at + 4 * h);
+      const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float& v = x[4 * h + i];
+        const float mine = __fmul_rn(v, cc[i]), other = __fmul_rn(y[4 * h + i], ss[i]);
+        v = low ? __fsub_rn(mine, other) : __fadd_rn(mine, other);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void bf16x8_to_f32(const uint4& w, float (&x)[8]) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(u[i] << 16);
+    x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+}
+
+// Two FP32 numbers to two E4M3 codes, a in the low byte: nearest even, infinities saturate, NaN is 0x7F.
+__device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ float2 e4m3x2_to_f32(uint32_t w) {
+  uint32_t h;
+  const uint16_t in = (uint16_t)w;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(in));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+// 2^e, e in [-126, 127]
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+#endif
+
+}  // namespace paged
+}  // namespace kvq
