@@ -1727,6 +1727,10 @@ int attn_tcgen05_kernel_launches(const kvq_cache_desc* d, int64_t cache_len, int
 
 static std::atomic<uint32_t> g_wait_budget{0};           // 0: the default, kTimeoutCycles
 void set_attn_wait_budget(uint32_t cycles) { g_wait_budget.store(cycles, std::memory_order_relaxed); }
+uint32_t attn_wait_budget() {
+  const uint32_t b = g_wait_budget.load(std::memory_order_relaxed);
+  return b ? b : kTimeoutCycles;
+}
 
 // Common tail of both entry points.  `rot_area` (rot_area_bytes() bytes, 256-byte aligned; null only when
 // there are no cached keys) receives the rotated queries; `slots` holds the partial results of split units.
@@ -1770,7 +1774,7 @@ static int launch_planned(const AttnArgs& a, const Plan& pl, int64_t qb, int64_t
   p.scale_log2 = a.softmax_scale * kLog2e;
   p.ax_coef = -a.softmax_scale / 24.0f;
   p.lse = a.lse; p.cached_mass = a.cached_mass; p.status = a.status_word;
-  { const uint32_t b = g_wait_budget.load(std::memory_order_relaxed); p.wait_budget = b ? b : kTimeoutCycles; }
+  p.wait_budget = attn_wait_budget();
   p.q_blocks = (int)qb; p.n_units = (int)nu; p.tiles = (int)tiles;
   p.partial = slots;
   p.ax_rows = rp.ax;

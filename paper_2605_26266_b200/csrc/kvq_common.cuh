@@ -87,8 +87,9 @@ bool attn_tcgen05_addressable(const AttnArgs& a);
 size_t attn_tcgen05_workspace_bytes(const kvq_cache_desc* d, int64_t cache_len, int64_t m_tokens, int64_t n_cur, bool pair, bool least = false);
 int attn_tcgen05_kernel_launches(const kvq_cache_desc* d, int64_t cache_len, int64_t m_tokens, int64_t n_cur, bool pair);
 int launch_attn_tcgen05(const AttnArgs& a);
-// Cycle budget of the tcgen05 kernel's device-side waits for later launches (0 = the default of about a second).
+// Cycle budget of the tensor-core kernels' device-side waits for later launches (0 = the default of about a second).
 void set_attn_wait_budget(uint32_t cycles);
+uint32_t attn_wait_budget();
 // Same kernel, partial results of split units in the library's built-in scratch buffer (no caller workspace).
 int launch_attn_tcgen05_static(const AttnArgs& a);
 

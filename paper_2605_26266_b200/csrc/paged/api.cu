@@ -66,6 +66,12 @@ int check_attn_sizes(const kvq_paged_cache* c, const kvq_paged_batch* s, int32_t
   return KVQ_OK;
 }
 
+size_t workspace_bytes_of(const kvq_paged_cache* c, const kvq_paged_batch* s, int32_t q_heads, int64_t m_tokens) {
+  if (m_tokens == 0 || s->batch == 0) return 0;
+  const int group = q_heads / c->kv_heads;
+  return few_supports(c->head_dim, group, m_tokens) ? few_workspace_bytes(c->head_dim, group, m_tokens) : 0;
+}
+
 }  // namespace
 }  // namespace paged
 }  // namespace kvq
@@ -109,7 +115,7 @@ int kvq_paged_attn_workspace_bytes(const kvq_paged_cache* cache, const kvq_paged
   const int r = check_attn_sizes(cache, seqs, q_heads, m_tokens, flags, false);
   if (r != KVQ_OK) return r;
   if (!out_bytes) return KVQ_ERR_INVALID_ARG;
-  *out_bytes = 0;
+  *out_bytes = workspace_bytes_of(cache, seqs, q_heads, m_tokens);
   return KVQ_OK;
 }
 
@@ -126,6 +132,11 @@ int kvq_paged_attn(const kvq_paged_cache* cache, const kvq_paged_batch* seqs, co
   if (m_tokens == 0 || seqs->batch == 0) return KVQ_OK;
   if ((r = check_tensor(q_bf16, q_strides)) != KVQ_OK) return r;
   if ((r = check_tensor(out_bf16, o_strides)) != KVQ_OK) return r;
+  const size_t need = workspace_bytes_of(cache, seqs, q_heads, m_tokens);
+  if (need > 0) {
+    if (!workspace || workspace_bytes < need) return KVQ_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return KVQ_ERR_ALIGNMENT;
+  }
   c.pool = pool_of(cache); c.seqs = seqs_of(seqs); c.head_dim = cache->head_dim;
   c.q_heads = q_heads; c.group = q_heads / cache->kv_heads;
   c.q = q_bf16; c.qs = q_strides; c.out = out_bf16; c.os = o_strides; c.m_tokens = m_tokens;

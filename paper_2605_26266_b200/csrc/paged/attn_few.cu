@@ -1,0 +1,606 @@
+// kvq_paged_attn for a few query rows: decoding steps, drafts of a few tokens.  Bound by the bytes of the cache.
+//
+// The m tokens of the G query heads of a key head are R = G m <= 32 rows that read the same keys, so keys are the long side of both products
+// and take the tensor cores' 128 rows:   S^T = K Q^T  (128 keys x R),   O^T = V^T P^T  (channels x R).
+// K and V go from their pages by TMA to shared memory and from there into the products as they are, in E4M3: nothing is expanded.  What is not
+// in 8 bits is cut into parts of 8 bits that are exact or nearly so, each a few more columns of the same product, which the byte-bound kernel
+// has room for: a query into three E4M3 numbers (13 bits), a weight into two (9 bits; as BF16, which the output is rounded to).
+//
+// Weights of a tile: with b = log2 of the page's value scale,
+//   x = scale log2e q.k + b - m + 5,   P = 2^x,   l += 2^(x - b),   out = sum P code / l
+// so that the value scale is in the weight and the running maximum m bounds what is multiplied.  m may be exceeded by 3 (P <= 2^8 of E4M3's 448)
+// before it is raised, which one barrier with a vote decides for a tile; sums stay in registers (l, a key a lane) and in TMEM (O^T) meanwhile.
+//
+// Work: the tiles (128 tokens) of all (sequence, key head) units in one line, cut evenly over the CTAs; lengths are on the device, so every CTA finds
+// its place in the line itself.  Units that are cut leave FP32 partial rows for the merge kernel.
+#include "tensor.cuh"
+
+namespace kvq {
+namespace paged {
+
+namespace {
+
+using namespace ptx;
+
+struct FewParams {
+  Pool pool;
+  Seqs seqs;
+  Rope rope;
+  const uint16_t* q; kvq_strides qs;
+  uint16_t* out; kvq_strides os;
+  int q_heads, group, m_tokens;
+  float scale_log2;
+  int causal, window;
+  float* lse;
+  int32_t* status;
+  uint8_t* slots;                  // partial rows
+  int4* headers;                   // [CTAs][2]: what a slot holds
+  uint32_t wait_budget;
+};
+
+constexpr int kThreads = 256;      // producer, issuer, two warps for rows without keys, four softmax warps
+constexpr float kBase = 5.f, kSlack = 3.f;
+enum { kNone = 0, kStart = 1, kMiddle = 2, kEnd = 3 };
+
+template <int D, int NR>
+struct Few {
+  static constexpr int kN = NR == 8 ? 32 : 3 * NR;                  // columns of S^T: three parts (a multiple of 16)
+  static constexpr int kNP = 2 * NR;                                // columns of O^T
+  static constexpr int kTile = kTileKeys * D;                       // bytes of a tile of keys or values
+  static constexpr int kStages = D == 128 ? 6 : 8;
+  static constexpr int kOffQ = kStages * 2 * kTile;
+  static constexpr int kOffP = kOffQ + (kN * D + 1023) / 1024 * 1024;
+  static constexpr int kPBytes = kTileKeys * kNP;
+  static constexpr int kOffBar = kOffP + 2 * kPBytes;
+  enum { kFull = 0, kEmpty = kFull + kStages, kQFull = kEmpty + kStages, kSFull, kSFree = kSFull + 2, kPFull = kSFree + 2, kPDone = kPFull + 2,
+         kDrain = kPDone + 2, kBars };
+  static constexpr int kOffMisc = kOffBar + kBars * 8;              // tmem base, abort
+  static constexpr int kOffScale = (kOffMisc + 8 + 15) / 16 * 16;   // [stages][2][8] scale bytes of a tile's pages
+  static constexpr int kOffRow = kOffScale + kStages * 16;          // floats: row factors, 5 - m, f, partial maxima and sums [4][NR]
+  static constexpr int kOffAcc = kOffRow + (3 + 4) * NR * 4;        // whether the product of a buffer adds to O^T
+  static constexpr int kOffWalk = (kOffAcc + 8 + 15) / 16 * 16;
+  static constexpr int kSmem = kOffWalk + 32 + 1024;
+  static constexpr int kTmemS = 0, kTmemO = 2 * kN;
+  static constexpr int kTmemCols = 2 * kN + kNP <= 128 ? 128 : 256;
+  static constexpr int kSlotBytes = NR * (D + 2) * 4;
+};
+
+// A CTA's place in the line of tiles.
+struct Place { int b, h, t; long long left; };
+struct Segment { int b, h, tb, te, n, first; Extent ex; };      // tiles [tb, te) of the unit's n, which begin with tile `first` of the sequence
+
+struct Walker {
+  Place at;
+  Extent ex;
+  Tiles tl;
+  bool known;
+  __device__ __forceinline__ Walker(const Place& p) : at(p), known(false) {}
+  __device__ __forceinline__ bool next(Segment& s, const FewParams& p) {
+    if (at.left <= 0) return false;
+    while (!known) {
+      ex = extent_of(p.seqs, p.pool.page, at.b, p.m_tokens, nullptr);
+      tl = tiles_of(ex, 0, p.m_tokens, p.causal, p.window);
+      if (tl.count > 0) known = true;
+      else ++at.b;
+    }
+    s.b = at.b; s.h = at.h; s.tb = at.t; s.n = tl.count; s.first = tl.first; s.ex = ex;
+    s.te = (int)min((long long)tl.count, at.t + at.left);
+    at.left -= s.te - s.tb;
+    at.t = 0;
+    if (++at.h == p.pool.kv_heads) { at.h = 0; ++at.b; known = false; }
+    return true;
+  }
+};
+
+// One warp: the place of CTA c of n in the line.
+__device__ __forceinline__ Place find_place(const FewParams& p, int c, int n) {
+  const int lane = threadIdx.x & 31;
+  auto tiles_at = [&](int b) -> long long {
+    if (b >= p.seqs.batch) return 0;
+    const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, p.status);
+    return (long long)tiles_of(ex, 0, p.m_tokens, p.causal, p.window).count * p.pool.kv_heads;
+  };
+  long long all = 0;
+  for (int b = lane; b < p.seqs.batch; b += 32) all += tiles_at(b);
+  for (int i = 16; i; i >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, i);
+  n = (int)min((long long)n, all);                       // so that no range between two others is empty
+  if (c >= n) return Place{0, 0, 0, 0};
+  const long long lo = all * c / n, hi = all * (c + 1) / n;
+  Place r{0, 0, 0, hi - lo};
+  long long before = 0;
+  for (int b0 = 0;; b0 += 32) {
+    const long long mine = tiles_at(b0 + lane);
+    long long upto = mine;
+    for (int i = 1; i < 32; i <<= 1) {
+      const long long o = __shfl_up_sync(0xFFFFFFFFu, upto, i);
+      if (lane >= i) upto += o;
+    }
+    const unsigned hit = __ballot_sync(0xFFFFFFFFu, before + upto > lo);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      const long long in = lo - before - __shfl_sync(0xFFFFFFFFu, upto - mine, src);
+      const int per = (int)(__shfl_sync(0xFFFFFFFFu, mine, src) / p.pool.kv_heads);
+      r.b = b0 + src; r.h = (int)(in / per); r.t = (int)(in % per);
+      return r;
+    }
+    before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+  }
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ bool barrier_or(uint32_t id, uint32_t n, bool x) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbar.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)x) : "memory");
+  return r != 0;
+}
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i + 32 <= N; i += 32) tmem_ld32(addr + i, r + i);
+  if constexpr (N % 32) tmem_ld16(addr + N / 32 * 32, r + N / 32 * 32);
+}
+
+template <int D, int NR>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const FewParams p) {
+  using F = Few<D, NR>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t sbase = smem_u32(smem);
+  volatile int* misc = reinterpret_cast<volatile int*>(smem + F::kOffMisc);
+  const Waits cx{sbase + F::kOffBar, misc + 1, p.wait_budget};
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    misc[1] = 0;
+    for (int s = 0; s < F::kStages; ++s) { mbar_init(cx.bar(F::kFull + s), 1); mbar_init(cx.bar(F::kEmpty + s), 1); }
+    mbar_init(cx.bar(F::kQFull), 128);
+    mbar_init(cx.bar(F::kDrain), 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(cx.bar(F::kSFull + s), 1); mbar_init(cx.bar(F::kSFree + s), 128);
+      mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kPDone + s), 1);
+    }
+    fence_barrier_init();
+    prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
+  }
+  // rows of the query tile that no part fills
+  for (int i = tid; i < F::kN * D / 16; i += kThreads) reinterpret_cast<uint4*>(smem + F::kOffQ)[i] = make_uint4(0, 0, 0, 0);
+  __syncwarp();
+  if (warp == 1) { tmem_alloc(sbase + F::kOffMisc, F::kTmemCols); tmem_relinquish(); }
+  wait_for_previous_grid();
+  allow_next_grid();
+  if (warp == 0) {
+    const Place pl = find_place(p, blockIdx.x, gridDim.x);
+    if (lane == 0) *reinterpret_cast<Place*>(smem + F::kOffWalk) = pl;
+  }
+  fence_proxy_async_smem();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + F::kOffMisc);
+  const Place place = *reinterpret_cast<const Place*>(smem + F::kOffWalk);
+
+  if (warp == 0) {
+    // ================= producer: pages of the tile's keys and values, and their scales =================
+    const int ppt = kTileKeys >> p.pool.log2_page;           // pages of a tile
+    Walker w(place);
+    Segment sg;
+    int it = 0;
+    bool ok = true;
+    while (ok && w.next(sg, p)) {
+      const int32_t* table = p.seqs.table + (int64_t)sg.b * p.seqs.table_stride;
+      const int total = sg.ex.before + sg.ex.fresh, last = (total - 1) >> p.pool.log2_page;      // last page of the sequence
+      // 32 pages at a time, a page a lane, a batch ahead: its number (one past the pool's end where there is none: the copy brings zeros)
+      // and its scale bytes (255: not seen)
+      auto fetch = [&](int page, int& id, uint32_t& scales) {
+        id = (int)p.pool.pages; scales = 0xFFFFu;
+        if (page <= last) {
+          const int n = load_coherent(table + page);
+          if (n < 0 || n >= p.pool.pages) {
+            report(p.status, kBadPage);
+          } else {
+            id = n;
+            const int64_t at = (int64_t)n * p.pool.kv_heads + sg.h;
+            scales = min((uint32_t)load_coherent(p.pool.k_scale + at), 254u) | min((uint32_t)load_coherent(p.pool.v_scale + at), 254u) << 8;
+          }
+        }
+      };
+      const int page0 = (sg.first + sg.tb) * ppt;
+      int id, id1;
+      uint32_t sc, sc1;
+      fetch(page0 + lane, id1, sc1);
+      id = id1; sc = sc1;
+      for (int t = sg.tb; t < sg.te; ++t, ++it) {
+        const int off = (t - sg.tb) * ppt;                   // pages of the segment so far
+        if ((off & 31) == 0) {
+          id = id1; sc = sc1;
+          fetch(page0 + off + 32 + lane, id1, sc1);
+        }
+        const int s = it % F::kStages;
+        ok = __all_sync(0xFFFFFFFFu, cx.wait(F::kEmpty + s, (it / F::kStages & 1) ^ 1, 601));
+        if (!ok) break;
+        const int from = (off & 31) + lane;
+        const int my_id = __shfl_sync(0xFFFFFFFFu, id, from & 31);
+        const uint32_t my_sc = __shfl_sync(0xFFFFFFFFu, sc, from & 31);
+        if (lane < ppt) {
+          smem[F::kOffScale + s * 16 + lane] = (uint8_t)my_sc;
+          smem[F::kOffScale + s * 16 + 8 + lane] = (uint8_t)(my_sc >> 8);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive_expect_tx(cx.bar(F::kFull + s), 2 * F::kTile);
+        __syncwarp();
+        if (lane < ppt) {
+          const uint32_t dst = sbase + s * 2 * F::kTile + lane * (F::kTile / ppt);
+          tma_load_4d(dst, &tm_k, cx.bar(F::kFull + s), 0, 0, sg.h, my_id);
+          tma_load_4d(dst + F::kTile, &tm_v, cx.bar(F::kFull + s), 0, 0, sg.h, my_id);
+        }
+      }
+    }
+    // what is in flight lands before the CTA goes
+    if (*cx.abort)
+      for (int k = max(it - F::kStages, 0); k < it; ++k) cx.drain(F::kFull + k % F::kStages, k / F::kStages & 1);
+  } else if (warp == 1) {
+    // ================= issuer =================
+    const bool leader = elect_one();
+    const uint32_t idesc_s = make_idesc_e4m3(128, F::kN, 0, 0), idesc_o = make_idesc_e4m3(128, F::kNP, 1, 1);
+    const uint64_t dk = make_smem_desc(sbase, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
+    const uint64_t dq = make_smem_desc(sbase + F::kOffQ, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
+    // values: channels contiguous (M), eight keys an atom.  Of 64 channels the same 64 stand for rows 64 to 127 too (stride 0).
+    const uint64_t dv = make_smem_desc(sbase + F::kTile, 0, RowLayout<D>::kAtom, RowLayout<D>::kKind);
+    // weights: 16 columns of a key contiguous, key after key; blocks of 16 columns one after the other
+    const uint64_t dp = make_smem_desc(sbase + F::kOffP, 128, kTileKeys * 16, kLayoutNone);
+    const volatile int* accumulate = reinterpret_cast<const volatile int*>(smem + F::kOffAcc);
+    Walker w(place);
+    Segment sg;
+    int it = 0, nseg = 0;
+    bool ok = true;
+    auto all = [](bool x) -> bool { return __all_sync(0xFFFFFFFFu, x); };      // the warp stays together, also on its way out
+    auto scores = [&](int i) {
+      const int s = i % F::kStages, buf = i & 1;
+      if (!all(cx.wait(F::kFull + s, i / F::kStages & 1, 611)) || !all(cx.wait(F::kSFree + buf, (i >> 1 & 1) ^ 1, 612))) return false;
+      tc_fence_after();
+      if (leader) {
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+          mma_e4m3_ss(tmem + F::kTmemS + buf * F::kN, dk + (uint64_t)((s * 2 * F::kTile + 32 * k) >> 4), dq + (uint64_t)(2 * k), idesc_s, k > 0);
+        tc_commit(cx.bar(F::kSFull + buf));
+      }
+      return true;
+    };
+    while (ok && w.next(sg, p)) {
+      if (!(ok = all(cx.wait(F::kQFull, nseg & 1, 613)))) break;
+      tc_fence_after();
+      if (!(ok = scores(it))) break;
+      for (int t = sg.tb; t < sg.te; ++t, ++it) {
+        if (t + 1 < sg.te && !(ok = scores(it + 1))) break;
+        const int s = it % F::kStages, buf = it & 1;
+        if (!(ok = all(cx.wait(F::kPFull + buf, it >> 1 & 1, 614)))) break;
+        tc_fence_after();
+        if (leader) {
+          const uint32_t add = (uint32_t)accumulate[buf];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)                      // 32 keys a step
+            mma_e4m3_ss(tmem + F::kTmemO, dv + (uint64_t)((s * 2 * F::kTile + 32 * k * D) >> 4),
+                        dp + (uint64_t)((buf * F::kPBytes + k * 512) >> 4), idesc_o, k > 0 ? 1u : add);
+          tc_commit(cx.bar(F::kEmpty + s));
+          tc_commit(cx.bar(F::kPDone + buf));
+        }
+        __syncwarp();
+      }
+      ++nseg;
+    }
+    if (leader) tc_commit(cx.bar(F::kDrain));             // whatever has been issued is done before TMEM and shared memory go
+    __syncwarp();
+    cx.drain(F::kDrain, 0);
+    // Commits arrive in no promised order: the last ones of every barrier are waited for before the CTA goes.
+    if (ok) {
+      for (int k = max(it - F::kStages, 0); k < it; ++k) cx.drain(F::kEmpty + k % F::kStages, k / F::kStages & 1);
+      for (int k = max(it - 2, 0); k < it; ++k) cx.drain(F::kPDone + (k & 1), k >> 1 & 1);
+    }
+  } else if (warp < 4) {
+    // ================= rows that see nothing =================
+    for (int b = blockIdx.x; b < p.seqs.batch; b += gridDim.x) {
+      const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, nullptr);
+      const int from = tiles_of(ex, 0, p.m_tokens, p.causal, p.window).count > 0 ? ex.fresh : 0;
+      const int n = (p.m_tokens - from) * p.q_heads;
+      for (int i = tid - 64; i < n * (D / 8); i += 64) {
+        const int row = i / (D / 8), h = row % p.q_heads, t = from + row / p.q_heads;
+        *reinterpret_cast<uint4*>(p.out + (int64_t)b * p.os.b + (int64_t)h * p.os.h + (int64_t)t * p.os.t + 8 * (i % (D / 8))) = make_uint4(0, 0, 0, 0);
+        if (p.lse && i % (D / 8) == 0) p.lse[((int64_t)b * p.q_heads + h) * p.m_tokens + t] = -INFINITY;
+      }
+    }
+  } else {
+    // ================= softmax: a key of the tile a thread =================
+    const int key = tid - 128, wq = warp & 3;
+    const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
+    float* rowf = reinterpret_cast<float*>(smem + F::kOffRow);      // factor of a row's scores
+    float* shift = rowf + NR;                                       // 5 - m
+    float* drop = shift + NR;                                       // 2^(old m - new m)
+    float* part = drop + NR;                                        // [4][NR]
+    volatile int* accumulate = reinterpret_cast<volatile int*>(smem + F::kOffAcc);
+    const int rows = p.group * p.m_tokens;
+    int4* header = p.headers + 2 * blockIdx.x;
+    if (key == 0 && p.headers) header[0] = header[1] = make_int4(kNone, 0, 0, 0);
+    Walker w(place);
+    Segment sg;
+    int it = 0, nseg = 0;
+    bool ok = true;
+    while (ok && w.next(sg, p)) {
+      // ---- the rows of this unit, in parts ----
+      const int total = sg.ex.before + sg.ex.fresh;
+#pragma unroll 1
+      for (int r0 = 0; r0 < NR; r0 += 128 / (D / 8)) {
+        const int r = r0 + key / (D / 8), j = key % (D / 8);
+        const int t = r / p.group, g = r - t * p.group;
+        const bool real = r < NR && t < sg.ex.fresh && r < rows;
+        float x[8] = {};
+        if (real)
+          bf16x8_to_f32(*reinterpret_cast<const uint4*>(p.q + (int64_t)sg.b * p.qs.b + (int64_t)(sg.h * p.group + g) * p.qs.h + (int64_t)t * p.qs.t + 8 * j), x);
+        if (p.rope.dim) {
+          const int64_t at = (int64_t)rope_row(p.rope, sg.b, real ? t : 0, sg.ex.before, real ? p.status : nullptr) * (p.rope.dim >> 1);
+          rotate8(x, p.rope.cos + at, p.rope.sin + at, p.rope, j);
+        }
+        const QueryParts<3> qp = query_parts<D, 3>(x);
+        if (r < NR) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(smem + F::kOffQ + RowLayout<D>::at(i * NR + r, 8 * j)) = qp.part[i];
+          if (j == 0) { rowf[r] = qp.factor * p.scale_log2; shift[r] = kBase + 1e30f; }
+        }
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(cx.bar(F::kQFull));
+      named_barrier_sync(1, 128);
+      float l[NR], o[NR];
+#pragma unroll
+      for (int r = 0; r < NR; ++r) l[r] = o[r] = 0.f;
+      bool fresh = true;                                            // nothing of this segment is in TMEM's O^T
+      for (int t = sg.tb; t < sg.te; ++t, ++it) {
+        const int s = it % F::kStages, buf = it & 1;
+        // A wait that gives up does not end a warp's turn at the barriers of the four: the vote below ends it for all.
+        ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kFull + s, it / F::kStages & 1, 621));      // the scales
+        const int pg = key >> p.pool.log2_page;
+        const uint32_t kb = smem[F::kOffScale + s * 16 + pg], vb = smem[F::kOffScale + s * 16 + 8 + pg];
+        const int j = (sg.first + t) * kTileKeys + key;             // the key's place in the sequence
+        const bool there = kb != 255 && j < total;
+        const float kf = pow2(scale_exponent(kb));
+        const int ve = scale_exponent(vb);
+        ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kSFull + buf, it >> 1 & 1, 622));
+        tc_fence_after();
+        float x[NR];
+        {
+          uint32_t raw[F::kN];
+          tmem_load<F::kN>(tmem + lane_addr + F::kTmemS + buf * F::kN, raw);
+          tmem_wait_ld();
+          tc_fence_before();
+          mbar_arrive(cx.bar(F::kSFree + buf));
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            const float a = fmaf(__uint_as_float(raw[2 * NR + r]), 0x1p-8f, fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r])));
+            x[r] = fmaf(a, rowf[r] * kf, (float)ve);
+          }
+        }
+        // keys that a row does not see; whole tiles that all rows see need no test
+        const int tile0 = (sg.first + t) * kTileKeys, seen = p.causal ? sg.ex.before + 1 : total;      // what the first row sees
+        if (tile0 + kTileKeys > seen || (p.window && tile0 <= sg.ex.before + sg.ex.fresh - 1 - p.window) || __any_sync(0xFFFFFFFFu, !there)) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            const int at = sg.ex.before + r / p.group;
+            if (!there || (p.causal && j > at) || (p.window && j <= at - p.window)) x[r] = -INFINITY;
+          }
+        }
+        bool over = false;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) over |= x[r] + shift[r] > kBase + kSlack;
+        if (barrier_or(1, 128, over || !ok)) {                      // a row's maximum has to be raised
+          if (barrier_or(1, 128, !ok)) { ok = false; break; }
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            const float m = warp_max(x[r]);
+            if (lane == 0) part[wq * NR + r] = m;
+          }
+          named_barrier_sync(1, 128);
+          if (key < NR) {
+            const float old = kBase - shift[key];
+            const float m = fmaxf(fmaxf(fmaxf(part[key], part[NR + key]), fmaxf(part[2 * NR + key], part[3 * NR + key])), old);
+            drop[key] = ex2(old - m);
+            shift[key] = kBase - m;
+          }
+          if (!fresh) ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + (buf ^ 1), (it - 1) >> 1 & 1, 623));
+          named_barrier_sync(1, 128);
+          if (!fresh) {
+            uint32_t raw[F::kNP];
+            tc_fence_after();
+            tmem_load<F::kNP>(tmem + lane_addr + F::kTmemO, raw);
+            tmem_wait_ld();
+            tc_fence_before();
+#pragma unroll
+            for (int r = 0; r < NR; ++r) o[r] += fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r]));
+          }
+#pragma unroll
+          for (int r = 0; r < NR; ++r) { o[r] *= drop[r]; l[r] *= drop[r]; }
+          fresh = true;
+        }
+        const float inv_v = pow2(max(-ve, -126));
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          x[r] = ex2(x[r] + shift[r]);
+          l[r] = fmaf(x[r], inv_v, l[r]);
+        }
+        ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + buf, (it >> 1 & 1) ^ 1, 624));      // the product that read this buffer
+        uint32_t hi[NR / 4], lo[NR / 4];
+#pragma unroll
+        for (int r = 0; r < NR; r += 2) {
+          const uint32_t h = e4m3x2(x[r], x[r + 1]);
+          const float2 back = e4m3x2_to_f32(h);
+          const uint32_t rest = e4m3x2((x[r] - back.x) * 16.f, (x[r + 1] - back.y) * 16.f);
+          if (r & 2) { hi[r / 4] |= h << 16; lo[r / 4] |= rest << 16; }
+          else { hi[r / 4] = h; lo[r / 4] = rest; }
+        }
+        uint4* dst = reinterpret_cast<uint4*>(smem + F::kOffP + buf * F::kPBytes + key * 16);
+        if constexpr (NR == 8) {
+          dst[0] = make_uint4(hi[0], hi[1], lo[0], lo[1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < NR / 16; ++i) {
+            dst[i * kTileKeys] = make_uint4(hi[4 * i], hi[4 * i + 1], hi[4 * i + 2], hi[4 * i + 3]);
+            dst[(NR / 16 + i) * kTileKeys] = make_uint4(lo[4 * i], lo[4 * i + 1], lo[4 * i + 2], lo[4 * i + 3]);
+          }
+        }
+        if (key == 0) accumulate[buf] = fresh ? 0 : 1;
+        fresh = false;
+        fence_proxy_async_smem();
+        tc_fence_before();
+        mbar_arrive(cx.bar(F::kPFull + buf));
+      }
+      // ---- the rows' sums: l over the 128 keys of a thread each, O^T from TMEM, a channel a thread ----
+      ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + ((it - 1) & 1), (it - 1) >> 1 & 1, 625));
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+#pragma unroll
+        for (int i = 16; i; i >>= 1) l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], i);
+        if (lane == 0) part[wq * NR + r] = l[r];
+      }
+      if (barrier_or(1, 128, !ok)) { ok = false; break; }
+      tc_fence_after();
+      {
+        uint32_t raw[F::kNP];
+        tmem_load<F::kNP>(tmem + lane_addr + F::kTmemO, raw);
+        tmem_wait_ld();
+        tc_fence_before();
+#pragma unroll
+        for (int r = 0; r < NR; ++r) o[r] += fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r]));
+      }
+      const bool whole = sg.tb == 0 && sg.te == sg.n;
+      const int slot = nseg == 0 ? 0 : 1;
+      float* to = whole ? nullptr : reinterpret_cast<float*>(p.slots + (size_t)(2 * blockIdx.x + slot) * F::kSlotBytes);
+      if (!whole && key == 0) header[slot] = make_int4(sg.tb == 0 ? kStart : sg.te == sg.n ? kEnd : kMiddle, sg.b, sg.h, sg.ex.fresh);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const int t = r / p.group, g = r - t * p.group;
+        if (r >= rows || t >= sg.ex.fresh) continue;
+        const float sum = part[r] + part[NR + r] + part[2 * NR + r] + part[3 * NR + r];
+        if (whole) {
+          const int h = sg.h * p.group + g;
+          if (key < D) p.out[(int64_t)sg.b * p.os.b + (int64_t)h * p.os.h + (int64_t)t * p.os.t + key] = (uint16_t)f32_to_bf16_bits(sum == 0.f ? 0.f : o[r] / sum);
+          if (p.lse && key == 0) p.lse[((int64_t)sg.b * p.q_heads + h) * p.m_tokens + t] = (log2f(sum) - shift[r]) * 0.6931471805599453f;
+        } else {
+          if (key < D) to[r * D + key] = o[r];
+          if (key == 0) { to[NR * D + r] = -shift[r]; to[NR * D + NR + r] = sum; }
+        }
+      }
+      named_barrier_sync(1, 128);                                   // shift and part are the next segment's now
+      ++nseg;
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, F::kTmemCols);
+    if (lane == 0 && misc[1] != 0) report(p.status, misc[1]);
+  }
+}
+
+// Joins the partial rows of a unit that was cut: block (c, r) row r of the unit that begins in CTA c and goes on in the next ones.
+template <int D, int NR>
+__global__ void __launch_bounds__(D) paged_few_merge_kernel(const FewParams p, int ctas) {
+  using F = Few<D, NR>;
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int c = blockIdx.x, r = blockIdx.y, d = threadIdx.x;
+  int slot = 0;
+  int4 hd = load_coherent(p.headers + 2 * c);
+  if (hd.x != kStart) { hd = load_coherent(p.headers + 2 * c + 1); slot = 1; }
+  const int t = r / p.group, g = r - t * p.group;
+  if (hd.x != kStart || t >= hd.w) return;
+  float m = -INFINITY, l = 0.f, o = 0.f;
+  for (int k = c;; ++k) {
+    const float* from = reinterpret_cast<const float*>(p.slots + (size_t)(2 * k + (k == c ? slot : 0)) * F::kSlotBytes);
+    const float mk = load_coherent(from + NR * D + r), lk = load_coherent(from + NR * D + NR + r), ok = load_coherent(from + r * D + d);
+    const float top = fmaxf(m, mk), a = ex2(m - top), b = ex2(mk - top);
+    l = l * a + lk * b;
+    o = o * a + ok * b;
+    m = top;
+    if (k > c && load_coherent(p.headers + 2 * k).x != kMiddle) break;
+    if (k + 1 == ctas) break;
+  }
+  const int h = hd.z * p.group + g;
+  p.out[(int64_t)hd.y * p.os.b + (int64_t)h * p.os.h + (int64_t)t * p.os.t + d] = (uint16_t)f32_to_bf16_bits(l == 0.f ? 0.f : o / l);
+  if (p.lse && d == 0) p.lse[((int64_t)hd.y * p.q_heads + h) * p.m_tokens + t] = (log2f(l) + m) * 0.6931471805599453f;
+}
+
+int rows_of(int group, int64_t m_tokens) {
+  const int64_t r = group * m_tokens;
+  return r <= 8 ? 8 : r <= 16 ? 16 : 32;
+}
+int slot_bytes(int head_dim, int nr) { return nr * (head_dim + 2) * 4; }
+
+template <int D, int NR>
+int launch(const AttnCall& c, const CUtensorMap& mk, const CUtensorMap& mv, const FewParams& p, int ctas) {
+  using F = Few<D, NR>;
+  static PerDevice set;
+  int dev = 0;
+  int r = current_device(&dev);
+  if (r != KVQ_OK) return r;
+  if (set.first(dev)) {
+    KVQ_CUDA_TRY(cudaFuncSetAttribute(paged_few_kernel<D, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
+    set.done(dev);
+  }
+  r = launch_after(true, 1, dim3(ctas), dim3(kThreads), F::kSmem, c.stream, paged_few_kernel<D, NR>, mk, mv, p);
+  if (r != KVQ_OK) return r;
+  return launch_after(true, 1, dim3(ctas, (unsigned)(c.group * c.m_tokens)), dim3(D), 0, c.stream, paged_few_merge_kernel<D, NR>, p, ctas);
+}
+
+size_t header_bytes(int ctas) { return ((size_t)ctas * 2 * sizeof(int4) + 255) / 256 * 256; }
+
+}  // namespace
+
+bool few_supports(int head_dim, int group, int64_t m_tokens) { return group * m_tokens <= kFewRows; }
+
+size_t few_workspace_bytes(int head_dim, int group, int64_t m_tokens) {
+  int sms = 0;
+  if (device_sm_count(&sms) != KVQ_OK) { sms = 148; (void)cudaGetLastError(); }
+  return header_bytes(sms) + (size_t)sms * 2 * slot_bytes(head_dim, rows_of(group, m_tokens));
+}
+
+int launch_attn_few(const AttnCall& c) {
+  int sms = 0;
+  int r = device_sm_count(&sms);
+  if (r != KVQ_OK) return r;
+  CUtensorMap mk, mv;
+  if ((r = make_pool_map(&mk, c.pool.k_codes, c.pool, c.head_dim)) != KVQ_OK) return r;
+  if ((r = make_pool_map(&mv, c.pool.v_codes, c.pool, c.head_dim)) != KVQ_OK) return r;
+  FewParams p;
+  p.pool = c.pool; p.seqs = c.seqs; p.rope = c.rope;
+  p.q = static_cast<const uint16_t*>(c.q); p.qs = c.qs;
+  p.out = static_cast<uint16_t*>(c.out); p.os = c.os;
+  p.q_heads = c.q_heads; p.group = c.group; p.m_tokens = (int)c.m_tokens;
+  p.scale_log2 = c.softmax_scale * 1.4426950408889634f;
+  p.causal = c.causal; p.window = (int)c.window; p.lse = c.lse; p.status = c.status;
+  p.headers = static_cast<int4*>(c.workspace);
+  p.slots = static_cast<uint8_t*>(c.workspace) + header_bytes(sms);
+  p.wait_budget = wait_budget();
+  const int nr = rows_of(c.group, c.m_tokens);
+  if (c.head_dim == 64) {
+    if (nr == 8) return launch<64, 8>(c, mk, mv, p, sms);
+    if (nr == 16) return launch<64, 16>(c, mk, mv, p, sms);
+    return launch<64, 32>(c, mk, mv, p, sms);
+  }
+  if (nr == 8) return launch<128, 8>(c, mk, mv, p, sms);
+  if (nr == 16) return launch<128, 16>(c, mk, mv, p, sms);
+  return launch<128, 32>(c, mk, mv, p, sms);
+}
+
+}  // namespace paged
+}  // namespace kvq

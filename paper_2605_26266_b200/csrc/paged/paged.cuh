@@ -61,6 +61,12 @@ struct AppendCall {
 int launch_append(const AppendCall& c);
 int launch_attn(const AttnCall& c);
 
+// A few query rows (of all query heads of a key head together).
+constexpr int kFewRows = 32;
+bool few_supports(int head_dim, int group, int64_t m_tokens);
+size_t few_workspace_bytes(int head_dim, int group, int64_t m_tokens);
+int launch_attn_few(const AttnCall& c);
+
 #ifdef __CUDACC__
 __device__ __forceinline__ void report(int32_t* status, int code) {
   if (status) atomicCAS(status, 0, code);
@@ -79,6 +85,18 @@ __device__ __forceinline__ Extent extent_of(const Seqs& s, int page, int b, int6
   if (before + fresh > room) fresh = room - before;
   if (bad) report(status, kBadLength);
   return {(int)before, (int)fresh};
+}
+
+// Key tiles are 128 tokens, counted from a sequence's first one.  Those that the queries [t0, t1) of a sequence look into.
+constexpr int kTileKeys = 128;
+struct Tiles { int first, count; };
+__device__ __forceinline__ Tiles tiles_of(const Extent& ex, int t0, int t1, bool causal, int window) {
+  t1 = min(t1, ex.fresh);
+  if (t1 <= t0) return {0, 0};
+  const int end = causal ? ex.before + t1 : ex.before + ex.fresh;
+  const int begin = window ? max(ex.before + t0 + 1 - window, 0) : 0;      // window <= 2^31 - 1, before + t0 + 1 >= 1: no overflow
+  const int first = begin / kTileKeys;
+  return {first, (end + kTileKeys - 1) / kTileKeys - first};
 }
 
 // Row of the rotation's tables for new token t of sequence b.
@@ -153,6 +171,8 @@ __device__ __forceinline__ float2 e4m3x2_to_f32(uint32_t w) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(in));
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
+// A scale byte as an exponent that pow2() takes.
+__device__ __forceinline__ int scale_exponent(uint32_t byte) { return max(min((int)byte, 254) - kExpBias, -126); }
 // 2^e, e in [-126, 127]
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 #endif

@@ -1,0 +1,103 @@
+// What the tensor-core kernels of the paged cache share: waits, E4M3 products, maps of the pool, rotated queries in E4M3 parts.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "paged.cuh"
+#include "sm100_ptx.cuh"
+
+namespace kvq {
+namespace paged {
+
+// Bounded waits, as in the kernels over the low-bit cache: a wait that gives up leaves its code, every role leaves at its next wait.
+struct Waits {
+  uint32_t bar0;
+  volatile int* abort;
+  uint32_t budget;
+  __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8u * i; }
+  __device__ __forceinline__ bool wait(int i, uint32_t parity, int code) const {
+    const uint32_t b = bar(i);
+    if (ptx::mbar_try_wait(b, parity)) return true;
+    const uint32_t t0 = (uint32_t)clock();
+    while (!ptx::mbar_try_wait(b, parity)) {
+      if (*abort) return false;
+      if ((uint32_t)clock() - t0 > budget) { *abort = code; return false; }
+    }
+    return true;
+  }
+  // On the way out: lets what is in flight land, whatever the abort word says.
+  __device__ __forceinline__ void drain(int i, uint32_t parity) const {
+    const uint32_t b = bar(i);
+    const uint32_t t0 = (uint32_t)clock();
+    while (!ptx::mbar_try_wait(b, parity) && (uint32_t)clock() - t0 < 2000000000u) {}
+  }
+};
+
+// kind::f8f6f4 with E4M3 operands and FP32 accumulation: formats 0.  Bit 15 / 16: A / B stored with its M / N channels contiguous.
+__host__ __device__ constexpr uint32_t make_idesc_e4m3(int m, int n, int a_mn_major, int b_mn_major) {
+  return (1u << 4) | ((uint32_t)a_mn_major << 15) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void mma_e4m3_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+constexpr uint32_t kLayoutSw64 = 4;
+
+// A row of D code bytes is one swizzle row: 128-byte swizzle for 128 channels, 64-byte for 64.
+template <int D>
+struct RowLayout {
+  static constexpr uint32_t kKind = D == 128 ? ptx::kLayoutSw128 : kLayoutSw64;
+  static constexpr uint32_t kAtom = 8 * D;                 // eight rows
+  // byte offset of channel c (a multiple of 8) of row r
+  static __device__ __forceinline__ uint32_t at(int r, int c) {
+    const uint32_t chunk = (uint32_t)(c >> 4) ^ (D == 128 ? (uint32_t)(r & 7) : (uint32_t)((r >> 1) & 3));
+    return (uint32_t)r * D + chunk * 16 + (c & 8);
+  }
+};
+
+// Tensor map of a pool's codes, [pages, kv_heads, page, head_dim] bytes, one page of one head a box.
+int make_pool_map(CUtensorMap* map, const void* codes, const Pool& pool, int head_dim);
+// Cycles a wait may take (kvq_set_wait_budget_cycles).
+uint32_t wait_budget();
+
+// A row of queries: 8 channels of a lane, D / 8 neighbouring lanes a row.  Rotated, scaled by a power of two to at most 448 and cut
+// into PARTS E4M3 numbers, part i of them times 2^(4 i); with two parts 9 bits of each channel (a BF16 that is not rotated is exact), with
+// three 13.  `factor` is what a product with the parts, those after the first times 2^-4 each, has to be multiplied by; it is NaN for a
+// row with a channel that is no finite number, whose scores then are none either.
+template <int PARTS>
+struct QueryParts {
+  uint2 part[PARTS];
+  float factor;
+};
+template <int D, int PARTS>
+__device__ __forceinline__ QueryParts<PARTS> query_parts(float (&x)[8]) {
+  QueryParts<PARTS> r;
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int i = D / 16; i; i >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, i));
+  const int e = max((int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u), -100);
+  const float f = pow2(-e);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] *= f;
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t lo = e4m3x2(x[4 * h], x[4 * h + 1]), hi = e4m3x2(x[4 * h + 2], x[4 * h + 3]);
+      w[h] = lo | hi << 16;
+      const float2 a = e4m3x2_to_f32(lo), b = e4m3x2_to_f32(hi);
+      x[4 * h] = (x[4 * h] - a.x) * 16.f; x[4 * h + 1] = (x[4 * h + 1] - a.y) * 16.f;
+      x[4 * h + 2] = (x[4 * h + 2] - b.x) * 16.f; x[4 * h + 3] = (x[4 * h + 3] - b.y) * 16.f;
+    }
+    r.part[p] = make_uint2(w[0], w[1]);
+  }
+  r.factor = top < 0x7F800000u ? pow2(e) : __int_as_float(0x7FC00000);
+  return r;
+}
+
+}  // namespace paged
+}  // namespace kvq
