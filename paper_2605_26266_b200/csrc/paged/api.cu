@@ -69,7 +69,7 @@ int check_attn_sizes(const kvq_paged_cache* c, const kvq_paged_batch* s, int32_t
 size_t workspace_bytes_of(const kvq_paged_cache* c, const kvq_paged_batch* s, int32_t q_heads, int64_t m_tokens) {
   if (m_tokens == 0 || s->batch == 0) return 0;
   const int group = q_heads / c->kv_heads;
-  return few_supports(c->head_dim, group, m_tokens) ? few_workspace_bytes(c->head_dim, group, m_tokens) : 0;
+  return few_supports(c->head_dim, group, m_tokens) ? few_workspace_bytes(c->head_dim, group, m_tokens) : chunk_workspace_bytes(c->head_dim);
 }
 
 }  // namespace

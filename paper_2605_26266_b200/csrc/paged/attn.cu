@@ -113,6 +113,7 @@ __global__ void __launch_bounds__(kWarps * 32) paged_attn_kernel(const AttnParam
 
 int launch_attn(const AttnCall& c) {
   if (few_supports(c.head_dim, c.group, c.m_tokens)) return launch_attn_few(c);
+  return launch_attn_chunk(c);
   AttnParams p;
   p.pool = c.pool; p.seqs = c.seqs; p.rope = c.rope;
   p.q = static_cast<const uint16_t*>(c.q); p.qs = c.qs;

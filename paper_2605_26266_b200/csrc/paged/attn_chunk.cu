@@ -1,0 +1,688 @@
+// kvq_paged_attn for chunks and prompts: query rows on the tensor cores' long side, bound by products and exponentials.
+//
+// The m tokens of the G query heads of a key head are rows t G + g; a unit is 256 of them (two query tiles of 128) of one sequence and key head, and
+// walks over the key tiles (128 tokens) that its rows see.
+//
+//   S = Q K^T   K is multiplied as it lies in its pages, in E4M3.  A rotated query goes in as two E4M3 numbers whose sum carries 9 bits (a BF16 has 8), so that
+//               the two products take the time of one in BF16 and nothing has to be expanded.
+//   O += P V    weights are FP16 (11 bits), so V is expanded to FP16, exactly, by four warps that have nothing else to do: cutting weights into E4M3 parts
+//               would put more instructions on the softmax warps, which are what a step waits for.
+//
+// With f = scale log2e 2^(e_q + e_k) and b = log2 of the page's value scale, one pair per 16 keys (the smallest page):
+//   x = f s + b - m + 4,   P = 2^x,   l += 2^(x - b),   out = sum P code / l
+// The running maximum m is raised, and O scaled, only when it has grown by more than 8, so P <= 2^12.
+//
+// Work: the tile steps of all units in one line, cut evenly over the CTAs (lengths are on the device: every CTA finds its place itself).  Units that
+// are cut leave FP32 partial rows for the merge kernel.
+#include "tensor.cuh"
+
+namespace kvq {
+namespace paged {
+
+namespace {
+
+using namespace ptx;
+
+struct ChunkParams {
+  Pool pool;
+  Seqs seqs;
+  Rope rope;
+  const uint16_t* q; kvq_strides qs;
+  uint16_t* out; kvq_strides os;
+  int q_heads, group, m_tokens;
+  float scale_log2;
+  int causal, window;
+  float* lse;
+  int32_t* status;
+  uint8_t* slots;                  // partial rows
+  int4* headers;                   // [CTAs][2]: what a slot holds
+  uint32_t wait_budget;
+};
+
+constexpr int kThreads = 512;      // producer, two issuers, padding rows; two softmax groups; expanding warps
+constexpr int kRows = 256;
+constexpr int kRegsIssue = 48, kRegsSoftmax = 192, kRegsExpand = 80;      // 128 (48 + 2 * 192 + 80) = 512 * 128
+constexpr float kBase = 4.f, kSlack = 8.f, kNoMax = -1e30f;
+enum { kNone = 0, kStart = 1, kMiddle = 2, kEnd = 3 };
+
+template <int D>
+struct Chunk {
+  static constexpr int kTile = kTileKeys * D;                       // bytes of a tile of codes, and of a part of a query tile
+  static constexpr int kKStages = 3, kRawStages = 2, kVStages = 2;
+  static constexpr int kOffQ = 0;                                   // [query tile][part]
+  static constexpr int kOffK = kOffQ + 4 * kTile;
+  static constexpr int kOffRaw = kOffK + kKStages * kTile;
+  static constexpr int kOffV = kOffRaw + kRawStages * kTile;        // FP16
+  static constexpr int kOffBar = kOffV + kVStages * 2 * kTile;
+  enum { kKFull = 0, kKEmpty = kKFull + kKStages, kRawFull = kKEmpty + kKStages, kRawEmpty = kRawFull + kRawStages, kVFull = kRawEmpty + kRawStages,
+         kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPFull = kSFull + 2, kODone = kPFull + 4,
+         kOFree = kODone + 2, kDrain = kOFree + 2, kBars = kDrain + 2 };
+  static constexpr int kOffMisc = kOffBar + kBars * 8;
+  static constexpr int kOffScale = (kOffMisc + 8 + 127) / 128 * 128;      // [8 tiles][3][8] floats: key factors, value exponents, their inverses
+  static constexpr int kOffRow = kOffScale + 8 * 96;                 // [2][256] floats: factors of the rows of a segment and the next one
+  static constexpr int kOffWalk = kOffRow + 2 * kRows * 4;
+  static constexpr int kSmem = kOffWalk + 48 + 1024;
+  static constexpr int kSlotStats = kRows * D * 4;
+  static constexpr int kSlotBytes = kSlotStats + 2 * kRows * 4;
+};
+
+// A row block of a sequence and a CTA's place in the line of tile steps.
+struct Place { int b, h, rb, t; long long left; };
+struct Segment { int b, h, rb, tb, te, n, first; Extent ex; };
+
+// Row blocks of a sequence, and the key tiles of one.
+__device__ __forceinline__ int blocks_of(const Extent& ex, int group) { return (int)(((long long)ex.fresh * group + kRows - 1) / kRows); }
+__device__ __forceinline__ Tiles block_tiles(const Extent& ex, int rb, const ChunkParams& p) {
+  const int rows = ex.fresh * p.group, r0 = rb * kRows, r1 = min(r0 + kRows, rows);
+  return tiles_of(ex, r0 / p.group, (r1 + p.group - 1) / p.group, p.causal, p.window);
+}
+
+struct Walker {
+  Place at;
+  Extent ex;
+  int blocks;
+  bool known;
+  __device__ __forceinline__ Walker(const Place& p) : at(p), blocks(0), known(false) {}
+  __device__ __forceinline__ bool next(Segment& s, const ChunkParams& p) {
+    if (at.left <= 0) return false;
+    Tiles tl{0, 0};
+    while (true) {
+      if (!known) { ex = extent_of(p.seqs, p.pool.page, at.b, p.m_tokens, nullptr); blocks = blocks_of(ex, p.group); known = true; }
+      if (at.rb < blocks) {
+        tl = block_tiles(ex, at.rb, p);
+        if (tl.count > 0) break;
+        ++at.rb;
+      }
+      if (at.rb >= blocks) {
+        at.rb = 0;
+        if (++at.h == p.pool.kv_heads || blocks == 0) { at.h = 0; ++at.b; known = false; }
+      }
+    }
+    s.b = at.b; s.h = at.h; s.rb = at.rb; s.tb = at.t; s.n = tl.count; s.first = tl.first; s.ex = ex;
+    s.te = (int)min((long long)tl.count, at.t + at.left);
+    at.left -= s.te - s.tb;
+    at.t = 0;
+    ++at.rb;
+    return true;
+  }
+};
+
+// One warp: the place of CTA c of n in the line.
+__device__ __forceinline__ Place find_place(const ChunkParams& p, int c, int n) {
+  const int lane = threadIdx.x & 31;
+  auto tiles_at = [&](int b, int32_t* status) -> long long {             // of one key head
+    if (b >= p.seqs.batch) return 0;
+    const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, status);
+    const int blocks = blocks_of(ex, p.group);
+    long long sum = 0;
+    for (int rb = 0; rb < blocks; ++rb) sum += block_tiles(ex, rb, p).count;
+    return sum;
+  };
+  long long all = 0;
+  for (int b = lane; b < p.seqs.batch; b += 32) all += tiles_at(b, p.status);
+  for (int i = 16; i; i >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, i);
+  all *= p.pool.kv_heads;
+  n = (int)min((long long)n, all);                       // so that no range between two others is empty
+  if (c >= n) return Place{0, 0, 0, 0, 0};
+  const long long lo = all * c / n, hi = all * (c + 1) / n;
+  Place r{0, 0, 0, 0, hi - lo};
+  long long before = 0;
+  for (int b0 = 0;; b0 += 32) {
+    const long long mine = tiles_at(b0 + lane, nullptr);
+    long long upto = mine * p.pool.kv_heads;
+    for (int i = 1; i < 32; i <<= 1) {
+      const long long o = __shfl_up_sync(0xFFFFFFFFu, upto, i);
+      if (lane >= i) upto += o;
+    }
+    const unsigned hit = __ballot_sync(0xFFFFFFFFu, before + upto > lo);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      const long long per = __shfl_sync(0xFFFFFFFFu, mine, src);
+      const long long in = lo - before - (__shfl_sync(0xFFFFFFFFu, upto, src) - per * p.pool.kv_heads);
+      r.b = b0 + src; r.h = (int)(in / per);
+      long long rest = in % per;
+      const Extent ex = extent_of(p.seqs, p.pool.page, r.b, p.m_tokens, nullptr);
+      for (;; ++r.rb) {
+        const int count = block_tiles(ex, r.rb, p).count;
+        if (rest < count) break;
+        rest -= count;
+      }
+      r.t = (int)rest;
+      return r;
+    }
+    before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+  }
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t w) {
+  uint32_t h;
+  const uint16_t in = (uint16_t)w;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(in));
+  return h;
+}
+__device__ __forceinline__ bool all_lanes(bool x) { return __all_sync(0xFFFFFFFFu, x); }
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const ChunkParams p) {
+  using F = Chunk<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t sbase = smem_u32(smem);
+  volatile int* misc = reinterpret_cast<volatile int*>(smem + F::kOffMisc);
+  const Waits cx{sbase + F::kOffBar, misc + 1, p.wait_budget};
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    misc[1] = 0;
+    for (int s = 0; s < F::kKStages; ++s) { mbar_init(cx.bar(F::kKFull + s), 1); mbar_init(cx.bar(F::kKEmpty + s), 2); }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(cx.bar(F::kRawFull + s), 1); mbar_init(cx.bar(F::kRawEmpty + s), 128);
+      mbar_init(cx.bar(F::kVFull + s), 128); mbar_init(cx.bar(F::kVEmpty + s), 2);
+      mbar_init(cx.bar(F::kQFull + s), 128); mbar_init(cx.bar(F::kSFull + s), 1);
+      mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kPFull + 2 + s), 128);
+      mbar_init(cx.bar(F::kODone + s), 1); mbar_init(cx.bar(F::kOFree + s), 128);
+      mbar_init(cx.bar(F::kDrain + s), 1);
+    }
+    mbar_init(cx.bar(F::kQEmpty), 2);
+    fence_barrier_init();
+    prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
+  }
+  __syncwarp();
+  if (warp == 1) { tmem_alloc(sbase + F::kOffMisc, 512); tmem_relinquish(); }
+  wait_for_previous_grid();
+  allow_next_grid();
+  if (warp == 0) {
+    const Place pl = find_place(p, blockIdx.x, gridDim.x);
+    if (lane == 0) *reinterpret_cast<Place*>(smem + F::kOffWalk) = pl;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + F::kOffMisc);
+  const Place place = *reinterpret_cast<const Place*>(smem + F::kOffWalk);
+  // TMEM columns: S0 [0,128) S1 [128,256) O0 [256, 256 + D) O1 [384, 384 + D); weights (FP16 pairs) over the first 64 columns of their scores.
+
+  if (warp < 4) {
+    setmaxnreg_dec<kRegsIssue>();
+    if (warp == 0) {
+      // ================= producer =================
+      const int ppt = kTileKeys >> p.pool.log2_page;           // pages of a tile
+      Walker w(place);
+      Segment sg;
+      int it = 0, raws = 0;
+      bool ok = true;
+      while (ok && w.next(sg, p)) {
+        const int32_t* table = p.seqs.table + (int64_t)sg.b * p.seqs.table_stride;
+        const int last = (sg.ex.before + sg.ex.fresh - 1) >> p.pool.log2_page;
+        // 32 pages at a time, a page a lane, a batch ahead; one past the pool's end where there is none: the copy brings zeros, and scale byte 255 hides them
+        auto fetch = [&](int page, int& id, uint32_t& scales) {
+          id = (int)p.pool.pages; scales = 0xFFFFu;
+          if (page <= last) {
+            const int n = load_coherent(table + page);
+            if (n < 0 || n >= p.pool.pages) {
+              report(p.status, kBadPage);
+            } else {
+              id = n;
+              const int64_t at = (int64_t)n * p.pool.kv_heads + sg.h;
+              scales = min((uint32_t)load_coherent(p.pool.k_scale + at), 254u) | min((uint32_t)load_coherent(p.pool.v_scale + at), 254u) << 8;
+            }
+          }
+        };
+        const int page0 = (sg.first + sg.tb) * ppt;
+        int id, id1;
+        uint32_t sc, sc1;
+        fetch(page0 + lane, id1, sc1);
+        id = id1; sc = sc1;
+        for (int t = sg.tb; t < sg.te; ++t, ++it) {
+          const int off = (t - sg.tb) * ppt;
+          if ((off & 31) == 0) {
+            id = id1; sc = sc1;
+            fetch(page0 + off + 32 + lane, id1, sc1);
+          }
+          const int my_id = __shfl_sync(0xFFFFFFFFu, id, (off + lane) & 31);
+          const uint32_t g_sc = __shfl_sync(0xFFFFFFFFu, sc, (off + (((lane & 7) << 4) >> p.pool.log2_page)) & 31);
+          const int ks = it % F::kKStages;
+          ok = all_lanes(cx.wait(F::kKEmpty + ks, (it / F::kKStages & 1) ^ 1, 701));
+          if (!ok) break;
+          // What 16 keys' scores and weights are multiplied by.  The entry's last readers were done before the scores of tile it - 3 were issued.
+          if (lane < 8) {
+            float* at = reinterpret_cast<float*>(smem + F::kOffScale) + (it & 7) * 24 + lane;
+            const uint32_t kb = g_sc & 0xFFu, vb = g_sc >> 8;
+            const int ve = scale_exponent(vb);
+            at[0] = kb == 255u ? 1.f : pow2(scale_exponent(kb));
+            at[8] = kb == 255u ? -INFINITY : (float)ve;
+            at[16] = kb == 255u ? 0.f : pow2(max(-ve, -126));
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive_expect_tx(cx.bar(F::kKFull + ks), F::kTile);
+          __syncwarp();
+          if (lane < ppt) tma_load_4d(sbase + F::kOffK + ks * F::kTile + lane * (F::kTile / ppt), &tm_k, cx.bar(F::kKFull + ks), 0, 0, sg.h, my_id);
+          const int rs = it & 1;
+          ok = all_lanes(cx.wait(F::kRawEmpty + rs, (it >> 1 & 1) ^ 1, 702));
+          if (!ok) { ++it; break; }                            // keys of this tile are on their way, values are not
+          if (lane == 0) mbar_arrive_expect_tx(cx.bar(F::kRawFull + rs), F::kTile);
+          __syncwarp();
+          if (lane < ppt) tma_load_4d(sbase + F::kOffRaw + rs * F::kTile + lane * (F::kTile / ppt), &tm_v, cx.bar(F::kRawFull + rs), 0, 0, sg.h, my_id);
+          raws = it + 1;
+        }
+      }
+      if (*cx.abort) {                                         // what is in flight lands before the CTA goes
+        for (int k = max(it - F::kKStages, 0); k < it; ++k) cx.drain(F::kKFull + k % F::kKStages, k / F::kKStages & 1);
+        for (int k = max(raws - 2, 0); k < raws; ++k) cx.drain(F::kRawFull + (k & 1), k >> 1 & 1);
+      }
+    } else if (warp <= 2) {
+      // ================= issuers: warp 1 + qt for query tile qt =================
+      const bool leader = elect_one();
+      const int qt = warp - 1;
+      const uint32_t idesc_s = make_idesc_e4m3(128, 128, 0, 0);
+      const uint32_t idesc_o = make_idesc_bf16(128, D, 0, 1) & ~((7u << 7) | (7u << 10));      // FP16
+      const uint64_t dq = make_smem_desc(sbase + F::kOffQ + qt * 2 * F::kTile, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
+      const uint64_t dk = make_smem_desc(sbase + F::kOffK, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
+      const uint64_t dv = make_smem_desc(sbase + F::kOffV, kTileKeys * 128, 1024, kLayoutSw128);
+      const uint32_t s_tmem = tmem + qt * 128, o_tmem = tmem + 256 + qt * 128;
+      Walker w(place);
+      Segment sg;
+      int it = 0, n = 0, nseg = 0, nact = 0;                   // tiles, tiles and segments of this query tile
+      bool ok = true;
+      auto scores = [&](int i, bool act, bool last) -> bool {  // of tile i
+        const int s = i % F::kKStages;
+        if (!all_lanes(cx.wait(F::kKFull + s, i / F::kKStages & 1, 711))) return false;
+        tc_fence_after();
+        if (leader) {
+          if (act) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int k = 0; k < D / 32; ++k)
+                mma_e4m3_ss(s_tmem, dq + (uint64_t)((part * F::kTile + 32 * k) >> 4), dk + (uint64_t)((s * F::kTile + 32 * k) >> 4), idesc_s, part + k > 0);
+            tc_commit(cx.bar(F::kSFull + qt));
+          }
+          tc_commit(cx.bar(F::kKEmpty + s));
+          if (last) tc_commit(cx.bar(F::kQEmpty));
+        }
+        __syncwarp();
+        return true;
+      };
+      while (ok && w.next(sg, p)) {
+        const bool act = sg.ex.fresh * p.group - sg.rb * kRows > qt * 128;
+        if (!(ok = all_lanes(cx.wait(F::kQFull + qt, nseg & 1, 712)))) break;
+        tc_fence_after();
+        if (!(ok = scores(it, act, sg.te - sg.tb == 1))) break;
+        for (int t = sg.tb; t < sg.te; ++t, ++it) {
+          const int s = it & 1;
+          if (!(ok = all_lanes(cx.wait(F::kVFull + s, it >> 1 & 1, 713)))) break;
+          if (act) {
+            if (t == sg.tb && !(ok = all_lanes(cx.wait(F::kOFree + qt, (nact & 1) ^ 1, 714)))) break;
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              if (!(ok = all_lanes(cx.wait(F::kPFull + 2 * hf + qt, n & 1, 715)))) break;
+              tc_fence_after();
+              if (leader) {
+#pragma unroll
+                for (int k = 4 * hf; k < 4 * hf + 4; ++k)      // 16 keys a step
+                  mma_ts(o_tmem, s_tmem + 8 * k, dv + (uint64_t)((s * 2 * F::kTile + k * 16 * 128) >> 4), idesc_o, t > sg.tb || k > 0);
+              }
+              __syncwarp();
+            }
+            if (!ok) break;
+          }
+          if (leader) {
+            if (act) tc_commit(cx.bar(F::kODone + qt));
+            tc_commit(cx.bar(F::kVEmpty + s));
+          }
+          __syncwarp();
+          if (act) ++n;
+          if (t + 1 < sg.te && !(ok = scores(it + 1, act, t + 2 == sg.te))) break;
+        }
+        ++nseg;
+        if (act) ++nact;
+      }
+      if (leader) tc_commit(cx.bar(F::kDrain + qt));           // whatever has been issued is done before TMEM and shared memory go
+      __syncwarp();
+      cx.drain(F::kDrain + qt, 0);
+      // Commits arrive in no promised order: the last ones of every barrier are waited for too.
+      if (ok) {
+        for (int k = max(it - F::kKStages, 0); k < it; ++k) cx.drain(F::kKEmpty + k % F::kKStages, k / F::kKStages & 1);
+        for (int k = max(it - 2, 0); k < it; ++k) cx.drain(F::kVEmpty + (k & 1), k >> 1 & 1);
+        if (n > 0) { cx.drain(F::kSFull + qt, (n - 1) & 1); cx.drain(F::kODone + qt, (n - 1) & 1); }
+        if (nseg > 0) cx.drain(F::kQEmpty, (nseg - 1) & 1);
+      }
+    } else {
+      // ================= rows that see nothing =================
+      for (int b = blockIdx.x; b < p.seqs.batch; b += gridDim.x) {
+        const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, nullptr);
+        const int blocks = blocks_of(ex, p.group);
+        // blocks without a tile write nothing: rows of theirs are all the rows there are (no key is seen by any)
+        const int from = blocks > 0 && block_tiles(ex, blocks - 1, p).count > 0 ? ex.fresh : 0;
+        const long long n = (long long)(p.m_tokens - from) * p.q_heads * (D / 8);
+        for (long long i = lane; i < n; i += 32) {
+          const int c = (int)(i % (D / 8));
+          const long long row = i / (D / 8);
+          const int h = (int)(row % p.q_heads), t = from + (int)(row / p.q_heads);
+          *reinterpret_cast<uint4*>(p.out + (int64_t)b * p.os.b + (int64_t)h * p.os.h + (int64_t)t * p.os.t + 8 * c) = make_uint4(0, 0, 0, 0);
+          if (p.lse && c == 0) p.lse[((int64_t)b * p.q_heads + h) * p.m_tokens + t] = -INFINITY;
+        }
+      }
+    }
+  } else if (warp < 12) {
+    // ================= softmax: a query row a thread =================
+    setmaxnreg_inc<kRegsSoftmax>();
+    const int qt = (warp - 4) >> 2, wq = warp & 3;
+    const int r256 = qt * 128 + wq * 32 + lane;
+    const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
+    const uint32_t s_addr = tmem + lane_addr + qt * 128, o_addr = tmem + lane_addr + 256 + qt * 128;
+    int4* header = p.headers + 2 * blockIdx.x;
+    if (tid == 128) header[0] = header[1] = make_int4(kNone, 0, 0, 0);
+    Walker w(place);
+    Segment sg;
+    int it = 0, n = 0, nseg = 0;
+    bool ok = true;
+    while (ok && w.next(sg, p)) {
+      const int rows = sg.ex.fresh * p.group - sg.rb * kRows;        // of this block and after it
+      if (rows <= qt * 128) { it += sg.te - sg.tb; ++nseg; continue; }
+      const int total = sg.ex.before + sg.ex.fresh;
+      const int row = sg.rb * kRows + r256, tok = row / p.group, g = row - tok * p.group;
+      const bool real = r256 < rows;
+      const int pos = sg.ex.before + tok;
+      const int hi = real ? (p.causal ? pos + 1 : total) : 0x7FFFFFFF, lo = real && p.window ? pos + 1 - p.window : 0;      // keys [lo, hi) are seen
+      float m = kNoMax, l = 0.f, rowf = 0.f;
+      for (int t = sg.tb; t < sg.te; ++t, ++it, ++n) {
+        ok = all_lanes(cx.wait(F::kSFull + qt, n & 1, 721));
+        if (!ok) break;
+        tc_fence_after();
+        if (t == sg.tb) rowf = reinterpret_cast<const float*>(smem + F::kOffRow)[(nseg & 1) * kRows + r256];
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) tmem_ld32(s_addr + c, s + c);
+        const float4* sc = reinterpret_cast<const float4*>(smem + F::kOffScale) + (it & 7) * 6;
+        float f[8], v[8];
+        {
+          const float4 a = sc[0], b = sc[1], c = sc[2], d = sc[3];
+          f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+          v[0] = c.x; v[1] = c.y; v[2] = c.z; v[3] = c.w; v[4] = d.x; v[5] = d.y; v[6] = d.z; v[7] = d.w;
+        }
+        // not 0: a hidden score is -inf, and -inf * 0 would be none (a row of no finite numbers is dealt with at the end)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = fmaxf(f[i] * rowf, 1.17549435e-38f);
+        tmem_wait_ld();
+        const int tile0 = (sg.first + t) * kTileKeys;
+        if (__any_sync(0xFFFFFFFFu, tile0 + kTileKeys > hi || tile0 < lo) || tile0 + kTileKeys > total) {
+          const int nv = min(hi, total) - tile0, nl = lo - tile0;
+#pragma unroll
+          for (int i = 0; i < 128; ++i)
+            if (i >= nv || i < nl) s[i] = 0xFF800000u;
+        }
+        float m_new = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float a = max3(__uint_as_float(s[16 * i]), __uint_as_float(s[16 * i + 1]), __uint_as_float(s[16 * i + 2]));
+          float b = max3(__uint_as_float(s[16 * i + 3]), __uint_as_float(s[16 * i + 4]), __uint_as_float(s[16 * i + 5]));
+          a = max3(a, __uint_as_float(s[16 * i + 6]), __uint_as_float(s[16 * i + 7]));
+          b = max3(b, __uint_as_float(s[16 * i + 8]), __uint_as_float(s[16 * i + 9]));
+          a = max3(a, __uint_as_float(s[16 * i + 10]), __uint_as_float(s[16 * i + 11]));
+          b = max3(b, __uint_as_float(s[16 * i + 12]), __uint_as_float(s[16 * i + 13]));
+          a = max3(a, __uint_as_float(s[16 * i + 14]), __uint_as_float(s[16 * i + 15]));
+          m_new = fmaxf(m_new, fmaf(fmaxf(a, b), f[i], v[i]));
+        }
+        if (__any_sync(0xFFFFFFFFu, m_new - m > kSlack)) {
+          if (t > sg.tb) {
+            ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 722));      // the last product on O
+            if (!ok) break;
+            tc_fence_after();
+            const float drop = ex2(m - m_new);
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t r[16];
+              tmem_ld16(o_addr + 16 * c, r);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * drop);
+              tmem_st16(o_addr + 16 * c, r);
+            }
+            l *= drop;
+          }
+          m = m_new;
+        }
+        const float* inv = reinterpret_cast<const float*>(sc + 4);
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+          for (int i = 4 * hf; i < 4 * hf + 4; ++i) {
+            const float2 f2 = make_float2(f[i], f[i]);
+            const float b = v[i] - m + kBase;
+            const float2 b2 = make_float2(b, b);
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+              const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[16 * i + j]), __uint_as_float(s[16 * i + j + 1])), f2, b2);
+              const float2 w2 = make_float2(ex2(x.x), ex2(x.y));
+              sum = __fadd2_rn(sum, w2);
+              s[8 * i + j / 2] = cvt_f16x2(w2.x, w2.y);
+            }
+            l = fmaf(sum.x + sum.y, inv[i], l);
+          }
+          tmem_st32(s_addr + 32 * hf, s + 32 * hf);
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(cx.bar(F::kPFull + 2 * hf + qt));
+        }
+      }
+      if (!ok) break;
+      // ---- the rows' results ----
+      ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 723));
+      if (!ok) break;
+      tc_fence_after();
+      if (!(rowf == rowf)) l = rowf;                             // a query that is no finite number
+      const bool whole = sg.tb == 0 && sg.te == sg.n;
+      const int slot = nseg == 0 ? 0 : 1;
+      uint8_t* to = p.slots + (size_t)(2 * blockIdx.x + slot) * F::kSlotBytes;
+      const float norm = l == 0.f ? 0.f : 1.f / l;
+      const int head = sg.h * p.group + g;
+      uint16_t* out = p.out + (int64_t)sg.b * p.os.b + (int64_t)head * p.os.h + (int64_t)tok * p.os.t;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        uint32_t r[32];
+        tmem_ld32(o_addr + c, r);
+        tmem_wait_ld();
+        if (c + 32 == D) {                                       // all of the row is in registers
+          tc_fence_before();
+          mbar_arrive(cx.bar(F::kOFree + qt));
+        }
+        if (!whole) {                                            // pieces of four channels, row after row
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            *reinterpret_cast<uint4*>(to + ((size_t)((c + i) / 4) * kRows + r256) * 16) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+        } else if (real) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            uint4 o;
+            o.x = cvt_bf16x2(__uint_as_float(r[i]) * norm, __uint_as_float(r[i + 1]) * norm);
+            o.y = cvt_bf16x2(__uint_as_float(r[i + 2]) * norm, __uint_as_float(r[i + 3]) * norm);
+            o.z = cvt_bf16x2(__uint_as_float(r[i + 4]) * norm, __uint_as_float(r[i + 5]) * norm);
+            o.w = cvt_bf16x2(__uint_as_float(r[i + 6]) * norm, __uint_as_float(r[i + 7]) * norm);
+            *reinterpret_cast<uint4*>(out + c + i) = o;
+          }
+        }
+      }
+      if (!whole) {
+        float* st = reinterpret_cast<float*>(to + F::kSlotStats);
+        st[r256] = m; st[kRows + r256] = l;
+        if (tid == 128) header[slot] = make_int4((sg.tb == 0 ? kStart : sg.te == sg.n ? kEnd : kMiddle) | sg.h << 2, sg.b, sg.rb, sg.ex.fresh);
+      } else if (real && p.lse) {
+        p.lse[((int64_t)sg.b * p.q_heads + head) * p.m_tokens + tok] = (log2f(l) + m - kBase) * 0.6931471805599453f;
+      }
+      ++nseg;
+    }
+    tc_fence_before();
+  } else {
+    // ================= expanding warps: queries of a segment to E4M3 parts, values of a tile to FP16 =================
+    setmaxnreg_dec<kRegsExpand>();
+    const int dt = tid - 384;
+    constexpr int kLanes = D / 8, kAtOnce = 128 / kLanes;
+    Walker w(place);
+    Segment sg;
+    int it = 0, nseg = 0;
+    bool ok = true;
+    while (ok && w.next(sg, p)) {
+      ok = all_lanes(cx.wait(F::kQEmpty, (nseg & 1) ^ 1, 731));
+      if (!ok) break;
+      const int j = dt % kLanes, rows = sg.ex.fresh * p.group;
+      float* rowf = reinterpret_cast<float*>(smem + F::kOffRow) + (nseg & 1) * kRows;
+#pragma unroll 1
+      for (int qt = 0; qt < 2; ++qt) {
+#pragma unroll 4
+        for (int r0 = 0; r0 < 128; r0 += kAtOnce) {
+          const int r = r0 + dt / kLanes, row = sg.rb * kRows + qt * 128 + r;
+          const int tok = row / p.group, g = row - tok * p.group;
+          const bool real = row < rows;
+          float x[8] = {};
+          if (real)
+            bf16x8_to_f32(*reinterpret_cast<const uint4*>(p.q + (int64_t)sg.b * p.qs.b + (int64_t)(sg.h * p.group + g) * p.qs.h + (int64_t)tok * p.qs.t + 8 * j), x);
+          if (p.rope.dim) {
+            const int64_t at = (int64_t)rope_row(p.rope, sg.b, real ? tok : 0, sg.ex.before, real ? p.status : nullptr) * (p.rope.dim >> 1);
+            rotate8(x, p.rope.cos + at, p.rope.sin + at, p.rope, j);
+          }
+          const QueryParts<2> qp = query_parts<D, 2, 1>(x);
+          uint8_t* to = smem + F::kOffQ + qt * 2 * F::kTile + RowLayout<D>::at(r, 8 * j);
+          *reinterpret_cast<uint2*>(to) = qp.part[0];
+          *reinterpret_cast<uint2*>(to + F::kTile) = qp.part[1];
+          if (j == 0) rowf[qt * 128 + r] = qp.factor * p.scale_log2;
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(cx.bar(F::kQFull + qt));
+      }
+      for (int t = sg.tb; t < sg.te; ++t, ++it) {
+        const int s = it & 1;
+        ok = all_lanes(cx.wait(F::kRawFull + s, it >> 1 & 1, 732));
+        if (!ok) break;
+        ok = all_lanes(cx.wait(F::kVEmpty + s, (it >> 1 & 1) ^ 1, 733));
+        if (!ok) break;
+        const uint8_t* raw = smem + F::kOffRaw + s * F::kTile;
+        uint8_t* to = smem + F::kOffV + s * 2 * F::kTile + dt * 128;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {                       // 16 channels of key dt
+          const uint4 u = *reinterpret_cast<const uint4*>(raw + RowLayout<D>::at(dt, 16 * c));
+          const uint4 a = make_uint4(e4m3x2_to_f16x2(u.x & 0xFFFFu), e4m3x2_to_f16x2(u.x >> 16), e4m3x2_to_f16x2(u.y & 0xFFFFu), e4m3x2_to_f16x2(u.y >> 16));
+          const uint4 b = make_uint4(e4m3x2_to_f16x2(u.z & 0xFFFFu), e4m3x2_to_f16x2(u.z >> 16), e4m3x2_to_f16x2(u.w & 0xFFFFu), e4m3x2_to_f16x2(u.w >> 16));
+          uint8_t* block = to + (c / 4) * (kTileKeys * 128);
+          *reinterpret_cast<uint4*>(block + (((2 * c) & 7) ^ (dt & 7)) * 16) = a;
+          *reinterpret_cast<uint4*>(block + (((2 * c + 1) & 7) ^ (dt & 7)) * 16) = b;
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(cx.bar(F::kRawEmpty + s));
+        mbar_arrive(cx.bar(F::kVFull + s));
+      }
+      ++nseg;
+    }
+  }
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+    if (lane == 0 && misc[1] != 0) report(p.status, misc[1]);
+  }
+}
+
+// Joins the partial rows of a unit that was cut: block (c, i) takes rows [32 i, 32 i + 32) of the unit that begins in CTA c and goes on in the next ones; a
+// row a lane, four channels at a time.
+template <int D>
+__global__ void __launch_bounds__(256) paged_chunk_merge_kernel(const ChunkParams p, int ctas) {
+  using F = Chunk<D>;
+  wait_for_previous_grid();
+  allow_next_grid();
+  const int c = blockIdx.x, r = blockIdx.y * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+  int slot = 0;
+  int4 hd = load_coherent(p.headers + 2 * c);
+  if ((hd.x & 3) != kStart) { hd = load_coherent(p.headers + 2 * c + 1); slot = 1; }
+  const int row = hd.z * kRows + r, tok = row / p.group, g = row - tok * p.group;
+  if ((hd.x & 3) != kStart || tok >= hd.w) return;
+  const int head = (hd.x >> 2) * p.group + g;
+  float m = -INFINITY;
+  int end = c;
+  for (int k = c; k < ctas; ++k) {
+    const uint8_t* from = p.slots + (size_t)(2 * k + (k == c ? slot : 0)) * F::kSlotBytes;
+    m = fmaxf(m, load_coherent(reinterpret_cast<const float*>(from + F::kSlotStats) + r));
+    end = k;
+    if (k > c && (load_coherent(p.headers + 2 * k).x & 3) != kMiddle) break;
+  }
+  float l = 0.f;
+  float4 o[D / 32] = {};
+  for (int k = c; k <= end; ++k) {
+    const uint8_t* from = p.slots + (size_t)(2 * k + (k == c ? slot : 0)) * F::kSlotBytes;
+    const float* st = reinterpret_cast<const float*>(from + F::kSlotStats);
+    const float a = ex2(load_coherent(st + r) - m);
+    l = fmaf(load_coherent(st + kRows + r), a, l);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const float4 x = load_coherent(reinterpret_cast<const float4*>(from) + (size_t)(warp * (D / 32) + i) * kRows + r);
+      o[i].x = fmaf(x.x, a, o[i].x); o[i].y = fmaf(x.y, a, o[i].y); o[i].z = fmaf(x.z, a, o[i].z); o[i].w = fmaf(x.w, a, o[i].w);
+    }
+  }
+  const float norm = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* out = p.out + (int64_t)hd.y * p.os.b + (int64_t)head * p.os.h + (int64_t)tok * p.os.t + warp * (D / 8);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+    *reinterpret_cast<uint2*>(out + 4 * i) = make_uint2(cvt_bf16x2(o[i].x * norm, o[i].y * norm), cvt_bf16x2(o[i].z * norm, o[i].w * norm));
+  if (p.lse && warp == 0) p.lse[((int64_t)hd.y * p.q_heads + head) * p.m_tokens + tok] = (log2f(l) + m - kBase) * 0.6931471805599453f;
+}
+
+size_t header_bytes(int ctas) { return ((size_t)ctas * 2 * sizeof(int4) + 255) / 256 * 256; }
+
+template <int D>
+int launch(const AttnCall& c, const CUtensorMap& mk, const CUtensorMap& mv, const ChunkParams& p, int ctas) {
+  using F = Chunk<D>;
+  static PerDevice set;
+  int dev = 0;
+  int r = current_device(&dev);
+  if (r != KVQ_OK) return r;
+  if (set.first(dev)) {
+    KVQ_CUDA_TRY(cudaFuncSetAttribute(paged_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
+    set.done(dev);
+  }
+  r = launch_after(true, 1, dim3(ctas), dim3(kThreads), F::kSmem, c.stream, paged_chunk_kernel<D>, mk, mv, p);
+  if (r != KVQ_OK) return r;
+  return launch_after(true, 1, dim3(ctas, kRows / 32), dim3(256), 0, c.stream, paged_chunk_merge_kernel<D>, p, ctas);
+}
+
+}  // namespace
+
+size_t chunk_workspace_bytes(int head_dim) {
+  int sms = 0;
+  if (device_sm_count(&sms) != KVQ_OK) { sms = 148; (void)cudaGetLastError(); }
+  return header_bytes(sms) + (size_t)sms * 2 * (head_dim == 64 ? Chunk<64>::kSlotBytes : Chunk<128>::kSlotBytes);
+}
+
+int launch_attn_chunk(const AttnCall& c) {
+  int sms = 0;
+  int r = device_sm_count(&sms);
+  if (r != KVQ_OK) return r;
+  CUtensorMap mk, mv;
+  if ((r = make_pool_map(&mk, c.pool.k_codes, c.pool, c.head_dim)) != KVQ_OK) return r;
+  if ((r = make_pool_map(&mv, c.pool.v_codes, c.pool, c.head_dim)) != KVQ_OK) return r;
+  ChunkParams p;
+  p.pool = c.pool; p.seqs = c.seqs; p.rope = c.rope;
+  p.q = static_cast<const uint16_t*>(c.q); p.qs = c.qs;
+  p.out = static_cast<uint16_t*>(c.out); p.os = c.os;
+  p.q_heads = c.q_heads; p.group = c.group; p.m_tokens = (int)c.m_tokens;
+  p.scale_log2 = c.softmax_scale * 1.4426950408889634f;
+  p.causal = c.causal; p.window = (int)c.window; p.lse = c.lse; p.status = c.status;
+  p.headers = static_cast<int4*>(c.workspace);
+  p.slots = static_cast<uint8_t*>(c.workspace) + header_bytes(sms);
+  p.wait_budget = wait_budget();
+  return c.head_dim == 64 ? launch<64>(c, mk, mv, p, sms) : launch<128>(c, mk, mv, p, sms);
+}
+
+}  // namespace paged
+}  // namespace kvq

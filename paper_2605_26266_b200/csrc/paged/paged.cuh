@@ -66,6 +66,8 @@ constexpr int kFewRows = 32;
 bool few_supports(int head_dim, int group, int64_t m_tokens);
 size_t few_workspace_bytes(int head_dim, int group, int64_t m_tokens);
 int launch_attn_few(const AttnCall& c);
+size_t chunk_workspace_bytes(int head_dim);
+int launch_attn_chunk(const AttnCall& c);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ void report(int32_t* status, int code) {

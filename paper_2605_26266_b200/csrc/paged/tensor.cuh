@@ -62,15 +62,15 @@ int make_pool_map(CUtensorMap* map, const void* codes, const Pool& pool, int hea
 uint32_t wait_budget();
 
 // A row of queries: 8 channels of a lane, D / 8 neighbouring lanes a row.  Rotated, scaled by a power of two to at most 448 and cut
-// into PARTS E4M3 numbers, part i of them times 2^(4 i); with two parts 9 bits of each channel (a BF16 that is not rotated is exact), with
-// three 13.  `factor` is what a product with the parts, those after the first times 2^-4 each, has to be multiplied by; it is NaN for a
+// into PARTS E4M3 numbers, part i of them times STEP^i (1 where one accumulator takes all parts); with two parts 9 bits of each channel (a BF16 that is not rotated is exact), with
+// three 13.  `factor` is what a product with the parts, part i divided by STEP^i, has to be multiplied by; it is NaN for a
 // row with a channel that is no finite number, whose scores then are none either.
 template <int PARTS>
 struct QueryParts {
   uint2 part[PARTS];
   float factor;
 };
-template <int D, int PARTS>
+template <int D, int PARTS, int STEP = 16>
 __device__ __forceinline__ QueryParts<PARTS> query_parts(float (&x)[8]) {
   QueryParts<PARTS> r;
   uint32_t top = 0;
@@ -90,8 +90,8 @@ __device__ __forceinline__ QueryParts<PARTS> query_parts(float (&x)[8]) {
       const uint32_t lo = e4m3x2(x[4 * h], x[4 * h + 1]), hi = e4m3x2(x[4 * h + 2], x[4 * h + 3]);
       w[h] = lo | hi << 16;
       const float2 a = e4m3x2_to_f32(lo), b = e4m3x2_to_f32(hi);
-      x[4 * h] = (x[4 * h] - a.x) * 16.f; x[4 * h + 1] = (x[4 * h + 1] - a.y) * 16.f;
-      x[4 * h + 2] = (x[4 * h + 2] - b.x) * 16.f; x[4 * h + 3] = (x[4 * h + 3] - b.y) * 16.f;
+      x[4 * h] = (x[4 * h] - a.x) * STEP; x[4 * h + 1] = (x[4 * h + 1] - a.y) * STEP;
+      x[4 * h + 2] = (x[4 * h + 2] - b.x) * STEP; x[4 * h + 3] = (x[4 * h + 3] - b.y) * STEP;
     }
     r.part[p] = make_uint2(w[0], w[1]);
   }
