@@ -36,13 +36,18 @@ struct ChunkParams {
   int32_t* status;
   uint8_t* slots;                  // partial rows
   int4* headers;                   // [CTAs][2]: what a slot holds
+  uint8_t* queries;                // [batch][key head][row block][query tile]: two parts of 128 rows as they lie in shared memory
+  float* factors;                  // [batch][key head][row block][256]
+  int max_blocks;                  // row blocks of m_tokens
+  int4* places;                    // [CTAs][2]: where a CTA's tile steps begin
+  long long* upto;                 // [batch]: tile steps of the sequences up to and with this one
   uint32_t wait_budget;
 };
 
-constexpr int kThreads = 512;      // producer, two issuers, padding rows; two softmax groups; expanding warps
+constexpr int kThreads = 512;      // producer, two issuers, queries; two softmax groups; expanding warps
 constexpr int kRows = 256;
-constexpr int kRegsIssue = 48, kRegsSoftmax = 192, kRegsExpand = 80;      // 128 (48 + 2 * 192 + 80) = 512 * 128
-constexpr float kBase = 4.f, kSlack = 8.f, kNoMax = -1e30f;
+constexpr int kRegsIssue = 72, kRegsSoftmax = 168, kRegsExpand = 104;      // 128 (72 + 2 * 168 + 104) = 512 * 128
+constexpr float kBase = 4.f, kSlack = 8.f, kNoMax = -1e30f, kLeast = 1.17549435e-38f;
 enum { kNone = 0, kStart = 1, kMiddle = 2, kEnd = 3 };
 
 template <int D>
@@ -55,13 +60,11 @@ struct Chunk {
   static constexpr int kOffV = kOffRaw + kRawStages * kTile;        // FP16
   static constexpr int kOffBar = kOffV + kVStages * 2 * kTile;
   enum { kKFull = 0, kKEmpty = kKFull + kKStages, kRawFull = kKEmpty + kKStages, kRawEmpty = kRawFull + kRawStages, kVFull = kRawEmpty + kRawStages,
-         kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPFull = kSFull + 2, kODone = kPFull + 4,
-         kOFree = kODone + 2, kDrain = kOFree + 2, kBars = kDrain + 2 };
+         kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPFull = kSFull + 4, kODone = kPFull + 4,
+         kOFree = kODone + 4, kDrain = kOFree + 2, kBars = kDrain + 2 };        // of scores, weights and products: + 2 half + query tile
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kOffScale = (kOffMisc + 8 + 127) / 128 * 128;      // [8 tiles][3][8] floats: key factors, value exponents, their inverses
-  static constexpr int kOffRow = kOffScale + 8 * 96;                 // [2][256] floats: factors of the rows of a segment and the next one
-  static constexpr int kOffWalk = kOffRow + 2 * kRows * 4;
-  static constexpr int kSmem = kOffWalk + 48 + 1024;
+  static constexpr int kSmem = kOffScale + 8 * 96 + 1024;
   static constexpr int kSlotStats = kRows * D * 4;
   static constexpr int kSlotBytes = kSlotStats + 2 * kRows * 4;
 };
@@ -107,50 +110,74 @@ struct Walker {
   }
 };
 
-// One warp: the place of CTA c of n in the line.
-__device__ __forceinline__ Place find_place(const ChunkParams& p, int c, int n) {
-  const int lane = threadIdx.x & 31;
-  auto tiles_at = [&](int b, int32_t* status) -> long long {             // of one key head
-    if (b >= p.seqs.batch) return 0;
-    const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, status);
-    const int blocks = blocks_of(ex, p.group);
-    long long sum = 0;
-    for (int rb = 0; rb < blocks; ++rb) sum += block_tiles(ex, rb, p).count;
-    return sum;
-  };
-  long long all = 0;
-  for (int b = lane; b < p.seqs.batch; b += 32) all += tiles_at(b, p.status);
-  for (int i = 16; i; i >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, i);
-  all *= p.pool.kv_heads;
-  n = (int)min((long long)n, all);                       // so that no range between two others is empty
-  if (c >= n) return Place{0, 0, 0, 0, 0};
-  const long long lo = all * c / n, hi = all * (c + 1) / n;
-  Place r{0, 0, 0, 0, hi - lo};
+// Row blocks of a sequence one after the other, without a division each.
+struct Blocks {
+  int t, rest, step, more, group, fresh;                       // the block's first row is token t, row `rest` of it
+  __device__ __forceinline__ Blocks(const Extent& ex, int g) : t(0), rest(0), step(kRows / g), more(kRows % g), group(g), fresh(ex.fresh) {}
+  __device__ __forceinline__ int next(const Extent& ex, const ChunkParams& p) {      // key tiles of this block
+    const int t0 = t;
+    t += step; rest += more;
+    if (rest >= group) { rest -= group; ++t; }
+    return tiles_of(ex, t0, t + (rest > 0), p.causal, p.window).count;
+  }
+};
+
+// One block: the line of tile steps (sequence, key head, row block, tile), cut evenly.
+__device__ void make_schedule(const ChunkParams& p, int ctas) {
+  __shared__ long long s_sum[kRows];
+  const int tid = threadIdx.x;
   long long before = 0;
-  for (int b0 = 0;; b0 += 32) {
-    const long long mine = tiles_at(b0 + lane, nullptr);
-    long long upto = mine * p.pool.kv_heads;
-    for (int i = 1; i < 32; i <<= 1) {
-      const long long o = __shfl_up_sync(0xFFFFFFFFu, upto, i);
-      if (lane >= i) upto += o;
-    }
-    const unsigned hit = __ballot_sync(0xFFFFFFFFu, before + upto > lo);
-    if (hit) {
-      const int src = __ffs(hit) - 1;
-      const long long per = __shfl_sync(0xFFFFFFFFu, mine, src);
-      const long long in = lo - before - (__shfl_sync(0xFFFFFFFFu, upto, src) - per * p.pool.kv_heads);
-      r.b = b0 + src; r.h = (int)(in / per);
-      long long rest = in % per;
-      const Extent ex = extent_of(p.seqs, p.pool.page, r.b, p.m_tokens, nullptr);
-      for (;; ++r.rb) {
-        const int count = block_tiles(ex, r.rb, p).count;
-        if (rest < count) break;
-        rest -= count;
+  for (int b0 = 0; b0 < p.seqs.batch; b0 += kRows) {
+    const int b = b0 + tid;
+    long long mine = 0;
+    if (b < p.seqs.batch) {
+      const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, nullptr);
+      const int blocks = blocks_of(ex, p.group);
+      if (p.causal) {
+        Blocks it(ex, p.group);
+        for (int rb = 0; rb < blocks; ++rb) mine += it.next(ex, p);
+      } else {
+        mine = (long long)blocks * tiles_of(ex, 0, 1, 0, 0).count;
       }
-      r.t = (int)rest;
-      return r;
     }
-    before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+    s_sum[tid] = mine * p.pool.kv_heads;
+    __syncthreads();
+    for (int i = 1; i < kRows; i <<= 1) {
+      const long long add = tid >= i ? s_sum[tid - i] : 0;
+      __syncthreads();
+      s_sum[tid] += add;
+      __syncthreads();
+    }
+    if (b < p.seqs.batch) p.upto[b] = before + s_sum[tid];
+    before += s_sum[kRows - 1];
+    __syncthreads();
+  }
+  const long long all = before, n = min((long long)ctas, all);      // no range between two others is empty
+  for (int c = tid; c < ctas; c += kRows) {
+    Place r{0, 0, 0, 0, 0};
+    if (c < n) {
+      const long long lo = all * c / n;
+      r.left = all * (c + 1) / n - lo;
+      int first = 0, last = p.seqs.batch - 1;                   // the first sequence with more than lo up to its end
+      while (first < last) {
+        const int mid = (first + last) >> 1;
+        if (load_coherent(p.upto + mid) > lo) last = mid; else first = mid + 1;
+      }
+      const long long start = first ? load_coherent(p.upto + first - 1) : 0, per = (load_coherent(p.upto + first) - start) / p.pool.kv_heads;
+      r.b = first;
+      r.h = (int)((lo - start) / per);
+      long long in = (lo - start) % per;
+      const Extent ex = extent_of(p.seqs, p.pool.page, r.b, p.m_tokens, nullptr);
+      Blocks it(ex, p.group);
+      for (;; ++r.rb) {
+        const int count = p.causal ? it.next(ex, p) : tiles_of(ex, 0, 1, 0, 0).count;
+        if (in < count) break;
+        in -= count;
+      }
+      r.t = (int)in;
+    }
+    p.places[2 * c] = make_int4(r.b, r.h, r.rb, r.t);
+    p.places[2 * c + 1] = make_int4((int)r.left, (int)(r.left >> 32), 0, 0);
   }
 }
 
@@ -170,7 +197,69 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t w) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(in));
   return h;
 }
+// tcgen05.wait::ld with the registers of a load that was issued long before: nothing that uses them may come ahead of it.
+__device__ __forceinline__ void tmem_wait_ld_of(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]),"+r"(r[1]),"+r"(r[2]),"+r"(r[3]),"+r"(r[4]),"+r"(r[5]),"+r"(r[6]),"+r"(r[7]),"+r"(r[8]),"+r"(r[9]),"+r"(r[10]),"+r"(r[11]),"+r"(r[12]),"+r"(r[13]),"+r"(r[14]),"+r"(r[15]),"+r"(r[16]),"+r"(r[17]),"+r"(r[18]),"+r"(r[19]),"+r"(r[20]),"+r"(r[21]),"+r"(r[22]),"+r"(r[23]),"+r"(r[24]),"+r"(r[25]),"+r"(r[26]),"+r"(r[27]),"+r"(r[28]),"+r"(r[29]),"+r"(r[30]),"+r"(r[31]) :: "memory");
+}
 __device__ __forceinline__ bool all_lanes(bool x) { return __all_sync(0xFFFFFFFFu, x); }
+
+// The queries of a call (and its schedule, by one block): rotated, in two E4M3 parts, laid out as the query tiles of the chunk kernel's units are in shared memory, so that one bulk copy
+// brings a tile.  A token's rotation is read once for the query heads of a key head.  (The four expanding warps of the chunk kernel did this between two
+// units; loads and shuffles of 256 rows one after the other held up the unit for longer than the rows take on the whole GPU.)
+constexpr int kQueryThreads = kRows;
+template <int D>
+__global__ void __launch_bounds__(kQueryThreads) paged_query_kernel(const ChunkParams p, int ctas) {
+  using F = Chunk<D>;
+  constexpr int kLanes = D / 8, kTokens = kQueryThreads / kLanes, kBatch = 4;
+  wait_for_previous_grid();
+  allow_next_grid();
+  if (blockIdx.x == 0) {                                     // ahead of the others: the chunk kernel waits for it too
+    if (blockIdx.y == 0 && blockIdx.z == 0) make_schedule(p, ctas);
+    return;
+  }
+  const int b = blockIdx.z, h = blockIdx.y, j = threadIdx.x % kLanes, t = ((int)blockIdx.x - 1) * kTokens + threadIdx.x / kLanes;
+  const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, p.status);
+  const int used = blocks_of(ex, p.group) * kRows;           // rows, those beyond the last token zeros
+  const bool real = t < ex.fresh;
+  // rows without a query answer nothing (every other row has a tile: it sees a key, or its block masks all of the tile)
+  if (!real && t < p.m_tokens) {
+    for (int g = 0; g < p.group; ++g) {
+      const int head = h * p.group + g;
+      *reinterpret_cast<uint4*>(p.out + (int64_t)b * p.os.b + (int64_t)head * p.os.h + (int64_t)t * p.os.t + 8 * j) = make_uint4(0, 0, 0, 0);
+      if (p.lse && j == 0) p.lse[((int64_t)b * p.q_heads + head) * p.m_tokens + t] = -INFINITY;
+    }
+  }
+  if ((long long)((int)blockIdx.x - 1) * kTokens * p.group >= used) return;
+  const int64_t at = p.rope.dim ? (int64_t)rope_row(p.rope, b, real ? t : 0, ex.before, real ? p.status : nullptr) * (p.rope.dim >> 1) : 0;
+  const uint16_t* q = p.q + (int64_t)b * p.qs.b + (int64_t)h * p.group * p.qs.h + (int64_t)t * p.qs.t + 8 * j;
+  const int64_t unit0 = ((int64_t)b * p.pool.kv_heads + h) * p.max_blocks;
+  for (int g0 = 0; g0 < p.group; g0 += kBatch) {
+    uint4 raw[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      raw[i] = make_uint4(0, 0, 0, 0);
+      if (real && g0 + i < p.group) raw[i] = *reinterpret_cast<const uint4*>(q + (int64_t)(g0 + i) * p.qs.h);
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (g0 + i >= p.group) break;
+      float x[8];
+      bf16x8_to_f32(raw[i], x);
+      if (p.rope.dim) rotate8(x, p.rope.cos + at, p.rope.sin + at, p.rope, j);
+      const QueryParts<2> qp = query_parts<D, 2, 1>(x);
+      const long long row = (long long)t * p.group + g0 + i;
+      if (row < used) {
+        const int64_t unit = unit0 + (row >> 8);
+        const int r = (int)row & 127, qt = (int)(row >> 7) & 1;
+        uint8_t* to = p.queries + (unit * 2 + qt) * (2 * F::kTile) + RowLayout<D>::at(r, 8 * j);
+        *reinterpret_cast<uint2*>(to) = qp.part[0];
+        *reinterpret_cast<uint2*>(to + F::kTile) = qp.part[1];
+        if (j == 0) p.factors[unit * kRows + (row & (kRows - 1))] = qp.factor * p.scale_log2;
+      }
+    }
+  }
+}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -189,10 +278,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     for (int s = 0; s < 2; ++s) {
       mbar_init(cx.bar(F::kRawFull + s), 1); mbar_init(cx.bar(F::kRawEmpty + s), 128);
       mbar_init(cx.bar(F::kVFull + s), 128); mbar_init(cx.bar(F::kVEmpty + s), 2);
-      mbar_init(cx.bar(F::kQFull + s), 128); mbar_init(cx.bar(F::kSFull + s), 1);
-      mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kPFull + 2 + s), 128);
-      mbar_init(cx.bar(F::kODone + s), 1); mbar_init(cx.bar(F::kOFree + s), 128);
-      mbar_init(cx.bar(F::kDrain + s), 1);
+      mbar_init(cx.bar(F::kQFull + s), 1); mbar_init(cx.bar(F::kOFree + s), 128); mbar_init(cx.bar(F::kDrain + s), 1);
+    }
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(cx.bar(F::kSFull + s), 1); mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kODone + s), 1);
     }
     mbar_init(cx.bar(F::kQEmpty), 2);
     fence_barrier_init();
@@ -202,16 +291,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   if (warp == 1) { tmem_alloc(sbase + F::kOffMisc, 512); tmem_relinquish(); }
   wait_for_previous_grid();
   allow_next_grid();
-  if (warp == 0) {
-    const Place pl = find_place(p, blockIdx.x, gridDim.x);
-    if (lane == 0) *reinterpret_cast<Place*>(smem + F::kOffWalk) = pl;
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + F::kOffMisc);
-  const Place place = *reinterpret_cast<const Place*>(smem + F::kOffWalk);
-  // TMEM columns: S0 [0,128) S1 [128,256) O0 [256, 256 + D) O1 [384, 384 + D); weights (FP16 pairs) over the first 64 columns of their scores.
+  const int4 at = load_coherent(p.places + 2 * blockIdx.x), left = load_coherent(p.places + 2 * blockIdx.x + 1);
+  const Place place{at.x, at.y, at.z, at.w, (long long)(uint32_t)left.x | (long long)left.y << 32};
+  // TMEM columns: S0 [0,128) S1 [128,256) O0 [256, 256 + D) O1 [384, 384 + D); a key tile is two halves of 64 keys with 64 columns each,
+  // and weights (FP16 pairs) lie over the first 32 columns of their half's scores.
 
   if (warp < 4) {
     setmaxnreg_dec<kRegsIssue>();
@@ -285,7 +372,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       // ================= issuers: warp 1 + qt for query tile qt =================
       const bool leader = elect_one();
       const int qt = warp - 1;
-      const uint32_t idesc_s = make_idesc_e4m3(128, 128, 0, 0);
+      const uint32_t idesc_s = make_idesc_e4m3(128, 64, 0, 0);
       const uint32_t idesc_o = make_idesc_bf16(128, D, 0, 1) & ~((7u << 7) | (7u << 10));      // FP16
       const uint64_t dq = make_smem_desc(sbase + F::kOffQ + qt * 2 * F::kTile, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
       const uint64_t dk = make_smem_desc(sbase + F::kOffK, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
@@ -295,55 +382,56 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       Segment sg;
       int it = 0, n = 0, nseg = 0, nact = 0;                   // tiles, tiles and segments of this query tile
       bool ok = true;
-      auto scores = [&](int i, bool act, bool last) -> bool {  // of tile i
-        const int s = i % F::kKStages;
-        if (!all_lanes(cx.wait(F::kKFull + s, i / F::kKStages & 1, 711))) return false;
-        tc_fence_after();
-        if (leader) {
-          if (act) {
-#pragma unroll
-            for (int part = 0; part < 2; ++part)
-#pragma unroll
-              for (int k = 0; k < D / 32; ++k)
-                mma_e4m3_ss(s_tmem, dq + (uint64_t)((part * F::kTile + 32 * k) >> 4), dk + (uint64_t)((s * F::kTile + 32 * k) >> 4), idesc_s, part + k > 0);
-            tc_commit(cx.bar(F::kSFull + qt));
-          }
-          tc_commit(cx.bar(F::kKEmpty + s));
-          if (last) tc_commit(cx.bar(F::kQEmpty));
-        }
-        __syncwarp();
-        return true;
-      };
+      // Per half of a tile: O += P V over its 64 keys, then at once the same half's scores of the next tile, into the columns that P has left: the tensor
+      // pipe executes one thread's products in order.  So a softmax group has the other half to work on while its next scores are computed.
       while (ok && w.next(sg, p)) {
         const bool act = sg.ex.fresh * p.group - sg.rb * kRows > qt * 128;
         if (!(ok = all_lanes(cx.wait(F::kQFull + qt, nseg & 1, 712)))) break;
-        tc_fence_after();
-        if (!(ok = scores(it, act, sg.te - sg.tb == 1))) break;
-        for (int t = sg.tb; t < sg.te; ++t, ++it) {
-          const int s = it & 1;
-          if (!(ok = all_lanes(cx.wait(F::kVFull + s, it >> 1 & 1, 713)))) break;
-          if (act) {
-            if (t == sg.tb && !(ok = all_lanes(cx.wait(F::kOFree + qt, (nact & 1) ^ 1, 714)))) break;
+        for (int t = sg.tb - 1; t < sg.te && ok; ++t) {
+          const bool product = t >= sg.tb, next = t + 1 < sg.te;
+          const int i1 = product ? it + 1 : it, s1 = i1 % F::kKStages, vs = it & 1;
+#pragma unroll 1
+          for (int hf = 0; hf < 2; ++hf) {
+            if (product) {
+              if (hf == 0 && !(ok = all_lanes(cx.wait(F::kVFull + vs, it >> 1 & 1, 713)))) break;
+              if (act) {
+                if (hf == 0 && t == sg.tb && !(ok = all_lanes(cx.wait(F::kOFree + qt, (nact & 1) ^ 1, 714)))) break;
+                if (!(ok = all_lanes(cx.wait(F::kPFull + 2 * hf + qt, n & 1, 715)))) break;
+                tc_fence_after();
+                if (leader) {
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              if (!(ok = all_lanes(cx.wait(F::kPFull + 2 * hf + qt, n & 1, 715)))) break;
+                  for (int k = 0; k < 4; ++k)                  // 16 keys a step
+                    mma_ts(o_tmem, s_tmem + 64 * hf + 8 * k, dv + (uint64_t)((vs * 2 * F::kTile + (4 * hf + k) * 16 * 128) >> 4), idesc_o, t > sg.tb || hf > 0 || k > 0);
+                  tc_commit(cx.bar(F::kODone + 2 * hf + qt));
+                }
+              }
+              if (hf == 1 && leader) tc_commit(cx.bar(F::kVEmpty + vs));
+              __syncwarp();
+            }
+            if (next) {
+              if (hf == 0 && !(ok = all_lanes(cx.wait(F::kKFull + s1, i1 / F::kKStages & 1, 711)))) break;
               tc_fence_after();
               if (leader) {
+                if (act) {
 #pragma unroll
-                for (int k = 4 * hf; k < 4 * hf + 4; ++k)      // 16 keys a step
-                  mma_ts(o_tmem, s_tmem + 8 * k, dv + (uint64_t)((s * 2 * F::kTile + k * 16 * 128) >> 4), idesc_o, t > sg.tb || k > 0);
+                  for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int k = 0; k < D / 32; ++k)
+                      mma_e4m3_ss(s_tmem + 64 * hf, dq + (uint64_t)((part * F::kTile + 32 * k) >> 4), dk + (uint64_t)((s1 * F::kTile + hf * 64 * D + 32 * k) >> 4), idesc_s, part + k > 0);
+                  tc_commit(cx.bar(F::kSFull + 2 * hf + qt));
+                }
+                if (hf == 1) {
+                  tc_commit(cx.bar(F::kKEmpty + s1));
+                  if (t + 2 == sg.te) tc_commit(cx.bar(F::kQEmpty));
+                }
               }
               __syncwarp();
             }
-            if (!ok) break;
           }
-          if (leader) {
-            if (act) tc_commit(cx.bar(F::kODone + qt));
-            tc_commit(cx.bar(F::kVEmpty + s));
+          if (product) {
+            ++it;
+            if (act) ++n;
           }
-          __syncwarp();
-          if (act) ++n;
-          if (t + 1 < sg.te && !(ok = scores(it + 1, act, t + 2 == sg.te))) break;
         }
         ++nseg;
         if (act) ++nact;
@@ -355,25 +443,30 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       if (ok) {
         for (int k = max(it - F::kKStages, 0); k < it; ++k) cx.drain(F::kKEmpty + k % F::kKStages, k / F::kKStages & 1);
         for (int k = max(it - 2, 0); k < it; ++k) cx.drain(F::kVEmpty + (k & 1), k >> 1 & 1);
-        if (n > 0) { cx.drain(F::kSFull + qt, (n - 1) & 1); cx.drain(F::kODone + qt, (n - 1) & 1); }
+        if (n > 0)
+          for (int hf = 0; hf < 2; ++hf) { cx.drain(F::kSFull + 2 * hf + qt, (n - 1) & 1); cx.drain(F::kODone + 2 * hf + qt, (n - 1) & 1); }
         if (nseg > 0) cx.drain(F::kQEmpty, (nseg - 1) & 1);
       }
     } else {
-      // ================= rows that see nothing =================
-      for (int b = blockIdx.x; b < p.seqs.batch; b += gridDim.x) {
-        const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, nullptr);
-        const int blocks = blocks_of(ex, p.group);
-        // blocks without a tile write nothing: rows of theirs are all the rows there are (no key is seen by any)
-        const int from = blocks > 0 && block_tiles(ex, blocks - 1, p).count > 0 ? ex.fresh : 0;
-        const long long n = (long long)(p.m_tokens - from) * p.q_heads * (D / 8);
-        for (long long i = lane; i < n; i += 32) {
-          const int c = (int)(i % (D / 8));
-          const long long row = i / (D / 8);
-          const int h = (int)(row % p.q_heads), t = from + (int)(row / p.q_heads);
-          *reinterpret_cast<uint4*>(p.out + (int64_t)b * p.os.b + (int64_t)h * p.os.h + (int64_t)t * p.os.t + 8 * c) = make_uint4(0, 0, 0, 0);
-          if (p.lse && c == 0) p.lse[((int64_t)b * p.q_heads + h) * p.m_tokens + t] = -INFINITY;
+      // ================= queries =================
+      Walker w(place);
+      Segment sg;
+      int nseg = 0;
+      while (w.next(sg, p)) {
+        if (!all_lanes(cx.wait(F::kQEmpty, (nseg & 1) ^ 1, 703))) break;      // the scores of the segment before are done
+        if (lane == 0) {
+          const int64_t unit = ((int64_t)sg.b * p.pool.kv_heads + sg.h) * p.max_blocks + sg.rb;
+#pragma unroll
+          for (int qt = 0; qt < 2; ++qt) {
+            mbar_arrive_expect_tx(cx.bar(F::kQFull + qt), 2 * F::kTile);
+            bulk_load(sbase + F::kOffQ + qt * 2 * F::kTile, p.queries + (unit * 2 + qt) * (2 * F::kTile), 2 * F::kTile, cx.bar(F::kQFull + qt));
+          }
         }
+        __syncwarp();
+        ++nseg;
       }
+      if (*cx.abort && nseg > 0)
+        for (int qt = 0; qt < 2; ++qt) cx.drain(F::kQFull + qt, (nseg - 1) & 1);
     }
   } else if (warp < 12) {
     // ================= softmax: a query row a thread =================
@@ -396,49 +489,45 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const bool real = r256 < rows;
       const int pos = sg.ex.before + tok;
       const int hi = real ? (p.causal ? pos + 1 : total) : 0x7FFFFFFF, lo = real && p.window ? pos + 1 - p.window : 0;      // keys [lo, hi) are seen
-      float m = kNoMax, l = 0.f, rowf = 0.f;
-      for (int t = sg.tb; t < sg.te; ++t, ++it, ++n) {
-        ok = all_lanes(cx.wait(F::kSFull + qt, n & 1, 721));
-        if (!ok) break;
+      float m = kNoMax, l = 0.f;
+      const float rowf = load_coherent(p.factors + (((int64_t)sg.b * p.pool.kv_heads + sg.h) * p.max_blocks + sg.rb) * kRows + r256);
+      uint32_t s[64];
+      float f[4], v[4], inv[4];
+      auto fetch = [&](uint32_t (&s)[64], int hf, int i) -> bool {                  // scores of half hf of this query tile's tile i
+        if (!all_lanes(cx.wait(F::kSFull + 2 * hf + qt, i & 1, 721))) return false;
         tc_fence_after();
-        if (t == sg.tb) rowf = reinterpret_cast<const float*>(smem + F::kOffRow)[(nseg & 1) * kRows + r256];
-        uint32_t s[128];
-#pragma unroll
-        for (int c = 0; c < 128; c += 32) tmem_ld32(s_addr + c, s + c);
-        const float4* sc = reinterpret_cast<const float4*>(smem + F::kOffScale) + (it & 7) * 6;
-        float f[8], v[8];
-        {
-          const float4 a = sc[0], b = sc[1], c = sc[2], d = sc[3];
-          f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-          v[0] = c.x; v[1] = c.y; v[2] = c.z; v[3] = c.w; v[4] = d.x; v[5] = d.y; v[6] = d.z; v[7] = d.w;
-        }
+        tmem_ld32(s_addr + 64 * hf, s);
+        tmem_ld32(s_addr + 64 * hf + 32, s + 32);
+        return true;
+      };
+      // masks, factors and the running maximum of half hf of tile t (the it-th of the CTA, the n-th of the query tile)
+      auto prepare = [&](uint32_t (&s)[64], int hf, int t, int it, int n) -> bool {
+        const float4* sc = reinterpret_cast<const float4*>(smem + F::kOffScale) + (it & 7) * 6 + hf;
+        const float4 f4 = sc[0], v4 = sc[2], i4 = sc[4];
         // not 0: a hidden score is -inf, and -inf * 0 would be none (a row of no finite numbers is dealt with at the end)
+        f[0] = fmaxf(f4.x * rowf, kLeast); f[1] = fmaxf(f4.y * rowf, kLeast); f[2] = fmaxf(f4.z * rowf, kLeast); f[3] = fmaxf(f4.w * rowf, kLeast);
+        v[0] = v4.x; v[1] = v4.y; v[2] = v4.z; v[3] = v4.w;
+        inv[0] = i4.x; inv[1] = i4.y; inv[2] = i4.z; inv[3] = i4.w;
+        tmem_wait_ld_of(s);
+        tmem_wait_ld_of(s + 32);
+        const int first = (sg.first + t) * kTileKeys + 64 * hf;
+        if (__any_sync(0xFFFFFFFFu, first + 64 > hi || first < lo) || first + 64 > total) {
+          const int nv = min(hi, total) - first, nl = lo - first;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = fmaxf(f[i] * rowf, 1.17549435e-38f);
-        tmem_wait_ld();
-        const int tile0 = (sg.first + t) * kTileKeys;
-        if (__any_sync(0xFFFFFFFFu, tile0 + kTileKeys > hi || tile0 < lo) || tile0 + kTileKeys > total) {
-          const int nv = min(hi, total) - tile0, nl = lo - tile0;
-#pragma unroll
-          for (int i = 0; i < 128; ++i)
+          for (int i = 0; i < 64; ++i)
             if (i >= nv || i < nl) s[i] = 0xFF800000u;
         }
         float m_new = m;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float a = max3(__uint_as_float(s[16 * i]), __uint_as_float(s[16 * i + 1]), __uint_as_float(s[16 * i + 2]));
-          float b = max3(__uint_as_float(s[16 * i + 3]), __uint_as_float(s[16 * i + 4]), __uint_as_float(s[16 * i + 5]));
-          a = max3(a, __uint_as_float(s[16 * i + 6]), __uint_as_float(s[16 * i + 7]));
-          b = max3(b, __uint_as_float(s[16 * i + 8]), __uint_as_float(s[16 * i + 9]));
-          a = max3(a, __uint_as_float(s[16 * i + 10]), __uint_as_float(s[16 * i + 11]));
-          b = max3(b, __uint_as_float(s[16 * i + 12]), __uint_as_float(s[16 * i + 13]));
-          a = max3(a, __uint_as_float(s[16 * i + 14]), __uint_as_float(s[16 * i + 15]));
-          m_new = fmaxf(m_new, fmaf(fmaxf(a, b), f[i], v[i]));
+        for (int i = 0; i < 4; ++i) {
+          auto at = [&](int j) { return __uint_as_float(s[16 * i + j]); };
+          const float a = max3(max3(at(0), at(1), at(2)), at(3), at(4)), b = max3(max3(at(5), at(6), at(7)), at(8), at(9));
+          const float c = max3(max3(at(10), at(11), at(12)), at(13), at(14));
+          m_new = fmaxf(m_new, fmaf(max3(a, b, fmaxf(c, at(15))), f[i], v[i]));
         }
         if (__any_sync(0xFFFFFFFFu, m_new - m > kSlack)) {
-          if (t > sg.tb) {
-            ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 722));      // the last product on O
-            if (!ok) break;
+          if (t > sg.tb || hf > 0) {
+            if (!all_lanes(cx.wait(F::kODone + 2 * (hf ^ 1) + qt, (n - (hf ^ 1)) & 1, 722))) return false;      // the last product on O
             tc_fence_after();
             const float drop = ex2(m - m_new);
 #pragma unroll 1
@@ -454,33 +543,39 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           }
           m = m_new;
         }
-        const float* inv = reinterpret_cast<const float*>(sc + 4);
+        return true;
+      };
+      auto weights = [&](uint32_t (&s)[64], int hf) {
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
+        for (int i = 0; i < 4; ++i) {
+          const float2 f2 = make_float2(f[i], f[i]);
+          const float b = v[i] - m + kBase;
+          const float2 b2 = make_float2(b, b);
+          float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int i = 4 * hf; i < 4 * hf + 4; ++i) {
-            const float2 f2 = make_float2(f[i], f[i]);
-            const float b = v[i] - m + kBase;
-            const float2 b2 = make_float2(b, b);
-            float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-              const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[16 * i + j]), __uint_as_float(s[16 * i + j + 1])), f2, b2);
-              const float2 w2 = make_float2(ex2(x.x), ex2(x.y));
-              sum = __fadd2_rn(sum, w2);
-              s[8 * i + j / 2] = cvt_f16x2(w2.x, w2.y);
-            }
-            l = fmaf(sum.x + sum.y, inv[i], l);
+          for (int j = 0; j < 16; j += 2) {
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[16 * i + j]), __uint_as_float(s[16 * i + j + 1])), f2, b2);
+            const float2 w2 = make_float2(ex2(x.x), ex2(x.y));
+            sum = __fadd2_rn(sum, w2);
+            s[8 * i + j / 2] = cvt_f16x2(w2.x, w2.y);
           }
-          tmem_st32(s_addr + 32 * hf, s + 32 * hf);
-          tmem_wait_st();
-          tc_fence_before();
-          mbar_arrive(cx.bar(F::kPFull + 2 * hf + qt));
+          l = fmaf(sum.x + sum.y, inv[i], l);
         }
+        tmem_st32(s_addr + 64 * hf, s);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(cx.bar(F::kPFull + 2 * hf + qt));
+      };
+#pragma unroll 1
+      for (int i = 0; i < 2 * (sg.te - sg.tb); ++i) {
+        const int hf = i & 1, t = sg.tb + (i >> 1);
+        if (!(ok = fetch(s, hf, n) && prepare(s, hf, t, it, n))) break;
+        weights(s, hf);
+        it += hf; n += hf;
       }
       if (!ok) break;
       // ---- the rows' results ----
-      ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 723));
+      ok = all_lanes(cx.wait(F::kODone + 2 + qt, (n - 1) & 1, 723));      // the last product: a second half
       if (!ok) break;
       tc_fence_after();
       if (!(rowf == rowf)) l = rowf;                             // a query that is no finite number
@@ -526,42 +621,14 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     }
     tc_fence_before();
   } else {
-    // ================= expanding warps: queries of a segment to E4M3 parts, values of a tile to FP16 =================
+    // ================= expanding warps: values of a tile to FP16 =================
     setmaxnreg_dec<kRegsExpand>();
     const int dt = tid - 384;
-    constexpr int kLanes = D / 8, kAtOnce = 128 / kLanes;
     Walker w(place);
     Segment sg;
-    int it = 0, nseg = 0;
+    int it = 0;
     bool ok = true;
     while (ok && w.next(sg, p)) {
-      ok = all_lanes(cx.wait(F::kQEmpty, (nseg & 1) ^ 1, 731));
-      if (!ok) break;
-      const int j = dt % kLanes, rows = sg.ex.fresh * p.group;
-      float* rowf = reinterpret_cast<float*>(smem + F::kOffRow) + (nseg & 1) * kRows;
-#pragma unroll 1
-      for (int qt = 0; qt < 2; ++qt) {
-#pragma unroll 4
-        for (int r0 = 0; r0 < 128; r0 += kAtOnce) {
-          const int r = r0 + dt / kLanes, row = sg.rb * kRows + qt * 128 + r;
-          const int tok = row / p.group, g = row - tok * p.group;
-          const bool real = row < rows;
-          float x[8] = {};
-          if (real)
-            bf16x8_to_f32(*reinterpret_cast<const uint4*>(p.q + (int64_t)sg.b * p.qs.b + (int64_t)(sg.h * p.group + g) * p.qs.h + (int64_t)tok * p.qs.t + 8 * j), x);
-          if (p.rope.dim) {
-            const int64_t at = (int64_t)rope_row(p.rope, sg.b, real ? tok : 0, sg.ex.before, real ? p.status : nullptr) * (p.rope.dim >> 1);
-            rotate8(x, p.rope.cos + at, p.rope.sin + at, p.rope, j);
-          }
-          const QueryParts<2> qp = query_parts<D, 2, 1>(x);
-          uint8_t* to = smem + F::kOffQ + qt * 2 * F::kTile + RowLayout<D>::at(r, 8 * j);
-          *reinterpret_cast<uint2*>(to) = qp.part[0];
-          *reinterpret_cast<uint2*>(to + F::kTile) = qp.part[1];
-          if (j == 0) rowf[qt * 128 + r] = qp.factor * p.scale_log2;
-        }
-        fence_proxy_async_smem();
-        mbar_arrive(cx.bar(F::kQFull + qt));
-      }
       for (int t = sg.tb; t < sg.te; ++t, ++it) {
         const int s = it & 1;
         ok = all_lanes(cx.wait(F::kRawFull + s, it >> 1 & 1, 732));
@@ -583,7 +650,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         mbar_arrive(cx.bar(F::kRawEmpty + s));
         mbar_arrive(cx.bar(F::kVFull + s));
       }
-      ++nseg;
     }
   }
   __syncthreads();
@@ -638,7 +704,21 @@ __global__ void __launch_bounds__(256) paged_chunk_merge_kernel(const ChunkParam
   if (p.lse && warp == 0) p.lse[((int64_t)hd.y * p.q_heads + head) * p.m_tokens + tok] = (log2f(l) + m - kBase) * 0.6931471805599453f;
 }
 
-size_t header_bytes(int ctas) { return ((size_t)ctas * 2 * sizeof(int4) + 255) / 256 * 256; }
+size_t rounded(size_t n) { return (n + 255) / 256 * 256; }
+// The workspace: headers, the schedule, partial rows, queries in parts, their factors.
+struct Areas { size_t places, upto, slots, queries, factors, end; };
+Areas areas_of(int ctas, int head_dim, int batch, int kv_heads, int64_t blocks) {
+  Areas a;
+  a.places = rounded((size_t)ctas * 2 * sizeof(int4));
+  a.upto = a.places + rounded((size_t)ctas * 2 * sizeof(int4));
+  a.slots = a.upto + rounded((size_t)batch * sizeof(long long));
+  a.queries = a.slots + (size_t)ctas * 2 * (head_dim == 64 ? Chunk<64>::kSlotBytes : Chunk<128>::kSlotBytes);
+  const size_t units = (size_t)batch * kv_heads * (size_t)blocks;
+  a.factors = a.queries + units * kRows * 2 * head_dim;
+  a.end = a.factors + rounded(units * kRows * sizeof(float));
+  return a;
+}
+int64_t max_blocks(int group, int64_t m_tokens) { return (m_tokens * group + kRows - 1) / kRows; }
 
 template <int D>
 int launch(const AttnCall& c, const CUtensorMap& mk, const CUtensorMap& mv, const ChunkParams& p, int ctas) {
@@ -651,6 +731,9 @@ int launch(const AttnCall& c, const CUtensorMap& mk, const CUtensorMap& mv, cons
     KVQ_CUDA_TRY(cudaFuncSetAttribute(paged_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
     set.done(dev);
   }
+  const int64_t tokens = ((int64_t)p.max_blocks * kRows + c.group - 1) / c.group, per = kQueryThreads / (D / 8);
+  r = launch_after(true, 1, dim3((unsigned)((tokens + per - 1) / per) + 1, c.pool.kv_heads, c.seqs.batch), dim3(kQueryThreads), 0, c.stream, paged_query_kernel<D>, p, ctas);
+  if (r != KVQ_OK) return r;
   r = launch_after(true, 1, dim3(ctas), dim3(kThreads), F::kSmem, c.stream, paged_chunk_kernel<D>, mk, mv, p);
   if (r != KVQ_OK) return r;
   return launch_after(true, 1, dim3(ctas, kRows / 32), dim3(256), 0, c.stream, paged_chunk_merge_kernel<D>, p, ctas);
@@ -658,10 +741,10 @@ int launch(const AttnCall& c, const CUtensorMap& mk, const CUtensorMap& mv, cons
 
 }  // namespace
 
-size_t chunk_workspace_bytes(int head_dim) {
+size_t chunk_workspace_bytes(int head_dim, int batch, int kv_heads, int group, int64_t m_tokens) {
   int sms = 0;
   if (device_sm_count(&sms) != KVQ_OK) { sms = 148; (void)cudaGetLastError(); }
-  return header_bytes(sms) + (size_t)sms * 2 * (head_dim == 64 ? Chunk<64>::kSlotBytes : Chunk<128>::kSlotBytes);
+  return areas_of(sms, head_dim, batch, kv_heads, max_blocks(group, m_tokens)).end;
 }
 
 int launch_attn_chunk(const AttnCall& c) {
@@ -678,8 +761,15 @@ int launch_attn_chunk(const AttnCall& c) {
   p.q_heads = c.q_heads; p.group = c.group; p.m_tokens = (int)c.m_tokens;
   p.scale_log2 = c.softmax_scale * 1.4426950408889634f;
   p.causal = c.causal; p.window = (int)c.window; p.lse = c.lse; p.status = c.status;
-  p.headers = static_cast<int4*>(c.workspace);
-  p.slots = static_cast<uint8_t*>(c.workspace) + header_bytes(sms);
+  p.max_blocks = (int)max_blocks(c.group, c.m_tokens);
+  const Areas a = areas_of(sms, c.head_dim, c.seqs.batch, c.pool.kv_heads, p.max_blocks);
+  uint8_t* ws = static_cast<uint8_t*>(c.workspace);
+  p.headers = reinterpret_cast<int4*>(ws);
+  p.places = reinterpret_cast<int4*>(ws + a.places);
+  p.upto = reinterpret_cast<long long*>(ws + a.upto);
+  p.slots = ws + a.slots;
+  p.queries = ws + a.queries;
+  p.factors = reinterpret_cast<float*>(ws + a.factors);
   p.wait_budget = wait_budget();
   return c.head_dim == 64 ? launch<64>(c, mk, mv, p, sms) : launch<128>(c, mk, mv, p, sms);
 }

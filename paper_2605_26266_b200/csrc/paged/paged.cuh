@@ -59,14 +59,13 @@ struct AppendCall {
 };
 
 int launch_append(const AppendCall& c);
-int launch_attn(const AttnCall& c);
 
 // A few query rows (of all query heads of a key head together).
 constexpr int kFewRows = 32;
 bool few_supports(int head_dim, int group, int64_t m_tokens);
 size_t few_workspace_bytes(int head_dim, int group, int64_t m_tokens);
 int launch_attn_few(const AttnCall& c);
-size_t chunk_workspace_bytes(int head_dim);
+size_t chunk_workspace_bytes(int head_dim, int batch, int kv_heads, int group, int64_t m_tokens);
 int launch_attn_chunk(const AttnCall& c);
 
 #ifdef __CUDACC__
