@@ -137,10 +137,12 @@ try:
         raise ImportError("_py_call is of another torch or Python")
     _py_call.bind(*(C.cast(f, C.c_void_p).value for f in (_quantize_append, _attn_workspace_bytes, _attn_corrected)))
     _append_call, _attn_call = _py_call.append, _py_call.attn
+    _py_call.bind_paged(*(C.cast(f, C.c_void_p).value for f in (lib.kvq_paged_append, lib.kvq_paged_attn_workspace_bytes, lib.kvq_paged_attn)))
+    _paged_append_call, _paged_attn_call = _py_call.paged_append, _py_call.paged_attn
 except ImportError:
     def _append_call(*_):
         return _NOT_PLAIN
-    _attn_call = _append_call
+    _attn_call = _paged_append_call = _paged_attn_call = _append_call
 
 
 class KvqError(RuntimeError):
@@ -404,6 +406,7 @@ class PagedCache:
         self.buffers = list(buffers)
         self.desc.k_codes, self.desc.v_codes, self.desc.k_scale, self.desc.v_scale = [b.data_ptr() for b in self.buffers]
         self._workspaces = {}
+        self._address = C.addressof(self.desc)
 
     def views(self):
         """The four buffers shaped [pages, kv_heads, ...]: codes as float8_e4m3fn, scales as bytes (2^(byte - 127))."""
@@ -470,6 +473,12 @@ def kvq_paged_append(cache: PagedCache, k, v, page_table, lengths, n_new=None, c
     """Writes new tokens k, v ([batch, kv_heads, n, head_dim] BF16, CUDA; n_new[b] of them are real) behind the `lengths` (int32
     [batch]) tokens that the sequences of `page_table` (int32 [batch, width]) hold.  cos, sin: float32 [rows, dim / 2], rotate the
     keys; positions: int32 [batch, n], the tables' rows of the tokens (default: their places in the sequence)."""
+    status = _paged_append_call(cache._address, k, v, page_table, lengths, n_new, cos, sin, positions, interleaved, status_word, _stream()) if k.is_cuda else _NOT_PLAIN
+    if status != _NOT_PLAIN:
+        if status:
+            _check(status, "kvq_paged_append")
+        return
+    # not a plain call: checked and raised here
     batch, n = k.shape[0], k.shape[2]
     assert k.shape == v.shape
     d = cache.desc
@@ -490,6 +499,23 @@ def kvq_paged_attn(cache: PagedCache, q, page_table, lengths, softmax_scale, n_n
                    positions=None, interleaved=False, out=None, lse=None, status_word=None):
     """Attention of the new tokens q ([batch, q_heads, m, head_dim] BF16, CUDA) over the tokens of their sequences, which have
     been appended; page_table, lengths, n_new, cos, sin, positions as for the append.  Returns `out` (allocated if not given)."""
+    if out is None and type(q) is torch.Tensor:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if out is not None and q.is_cuda:
+        stream = _stream()
+        ws = cache._workspaces.get(stream) if cache._workspaces and not _capturing() else None
+        flags = KVQ_PAGED_CAUSAL if causal else 0
+        for _ in range(2):
+            status = _paged_attn_call(cache._address, q, page_table, lengths, n_new, cos, sin, positions, interleaved, out, softmax_scale, window, flags, lse, ws,
+                                      status_word, stream)
+            if status <= 0:
+                break
+            ws = cache._workspace(status, stream, q.device)
+        if status == KVQ_OK:
+            return out
+        if status != _NOT_PLAIN:
+            _check(status, "kvq_paged_attn")
+    # not a plain call: checked and raised here
     batch, heads, m, head_dim = q.shape
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)

@@ -1,4 +1,4 @@
-// CPython extension behind binding.py: the two calls of the hot path with their arguments taken straight from the tensor
+// CPython extension behind binding.py: the calls of the hot path with their arguments taken straight from the tensor
 // objects.  Through ctypes a call is 30 to 60 Python-level operations (attributes, strides as a struct, data pointers, argument
 // conversion), and a small call is all host time: append of 2 heads x 256 tokens 5.7 us, of which 2.4 on the GPU.
 //
@@ -113,10 +113,143 @@ PyObject* attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLongLong(r);
 }
 
+// ---- the paged cache ----
+
+decltype(&kvq_paged_append) g_paged_append;
+decltype(&kvq_paged_attn_workspace_bytes) g_paged_workspace_bytes;
+decltype(&kvq_paged_attn) g_paged_attn;
+
+PyObject* bind_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  long long p[3];
+  for (int i = 0; i < 3; ++i)
+    if (n != 3 || !integer(a[i], &p[i])) { PyErr_SetString(PyExc_TypeError, "bind_paged(append, workspace_bytes, attn): addresses"); return nullptr; }
+  g_paged_append = reinterpret_cast<decltype(g_paged_append)>(p[0]);
+  g_paged_workspace_bytes = reinterpret_cast<decltype(g_paged_workspace_bytes)>(p[1]);
+  g_paged_attn = reinterpret_cast<decltype(g_paged_attn)>(p[2]);
+  Py_RETURN_NONE;
+}
+
+// Strides as binding.py's _paged_strides: those of a dimension of one element are made plain.
+kvq_strides paged_strides(const at::Tensor& t) {
+  return {t.size(0) > 1 ? t.stride(0) : 0, t.size(1) > 1 ? t.stride(1) : 0, t.size(2) > 1 ? t.stride(2) : t.size(3)};
+}
+const at::Tensor* cuda_tensor(PyObject* o, at::ScalarType type, int64_t dim) {
+  if (!THPVariable_CheckExact(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  return t.scalar_type() == type && t.is_cuda() && t.dim() == dim ? &t : nullptr;
+}
+// page_table, lengths, n_new (or None) of `batch` sequences
+bool paged_batch(PyObject* const* a, int64_t batch, kvq_paged_batch* s) {
+  const at::Tensor *table = cuda_tensor(a[0], at::kInt, 2), *lengths = cuda_tensor(a[1], at::kInt, 1);
+  const at::Tensor* fresh = a[2] == Py_None ? nullptr : cuda_tensor(a[2], at::kInt, 1);
+  if (!table || !lengths || (a[2] != Py_None && !fresh)) return false;
+  if (table->size(0) != batch || (table->size(1) > 1 && table->stride(1) != 1) || lengths->size(0) != batch || !lengths->is_contiguous()) return false;
+  if (fresh && (fresh->size(0) != batch || !fresh->is_contiguous())) return false;
+  const int64_t width = table->size(1);
+  if (batch > 0x7FFFFFFF || width > 0x7FFFFFFF) return false;
+  *s = {(int32_t)batch, (int32_t)width, batch > 1 ? table->stride(0) : width, static_cast<const int32_t*>(table->data_ptr()),
+        static_cast<const int32_t*>(lengths->data_ptr()), fresh ? static_cast<const int32_t*>(fresh->data_ptr()) : nullptr};
+  return true;
+}
+// cos, sin, positions (each or None), interleaved; *use: whether there is a rotation
+bool paged_rope(PyObject* const* a, int64_t batch, int64_t tokens, kvq_rope* r, bool* use) {
+  *use = a[0] != Py_None;
+  if (a[3] != Py_True && a[3] != Py_False) return false;
+  if (!*use) return a[1] == Py_None && a[2] == Py_None;
+  const at::Tensor *c = cuda_tensor(a[0], at::kFloat, 2), *s = cuda_tensor(a[1], at::kFloat, 2);
+  const at::Tensor* pos = a[2] == Py_None ? nullptr : cuda_tensor(a[2], at::kInt, 2);
+  if (!c || !s || c->sizes() != s->sizes() || !c->is_contiguous() || !s->is_contiguous() || (a[2] != Py_None && !pos)) return false;
+  if (pos && (pos->size(0) != batch || pos->size(1) != tokens || (tokens > 1 && pos->stride(1) != 1))) return false;
+  if (c->size(0) > 0x7FFFFFFF || c->size(1) > 0x3FFFFFFF) return false;
+  *r = {static_cast<const float*>(c->data_ptr()), static_cast<const float*>(s->data_ptr()), pos ? static_cast<const int32_t*>(pos->data_ptr()) : nullptr,
+        pos && batch > 1 ? pos->stride(0) : tokens, (int32_t)c->size(0), (int32_t)(2 * c->size(1)), a[3] == Py_True ? KVQ_ROPE_INTERLEAVED : 0u};
+  return true;
+}
+bool paged_status(PyObject* o, int32_t** out) {
+  *out = nullptr;
+  if (o == Py_None) return true;
+  if (!THPVariable_CheckExact(o)) return false;
+  *out = static_cast<int32_t*>(THPVariable_Unpack(o).data_ptr());
+  return true;
+}
+
+// paged_append(desc address, k, v, page_table, lengths, n_new, cos, sin, positions, interleaved, status, stream) -> status or kNotPlain
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  long long desc, stream, r = kNotPlain;
+  try {
+    if (n == 12 && g_paged_append && integer(a[0], &desc) && integer(a[11], &stream)) {
+      const kvq_paged_cache* d = reinterpret_cast<const kvq_paged_cache*>(desc);
+      const at::Tensor *k = plain(a[1]), *v = plain(a[2]);
+      kvq_paged_batch s;
+      kvq_rope rope;
+      bool turn;
+      int32_t* status;
+      if (k && v && k->sizes() == v->sizes() && k->size(1) == d->kv_heads && k->size(3) == d->head_dim && paged_batch(a + 3, k->size(0), &s) &&
+          paged_rope(a + 6, k->size(0), k->size(2), &rope, &turn) && paged_status(a[10], &status)) {
+        const void *kp = k->data_ptr(), *vp = v->data_ptr();
+        const kvq_strides ks = paged_strides(*k), vs = paged_strides(*v);
+        const int64_t tokens = k->size(2);
+        Py_BEGIN_ALLOW_THREADS
+        r = g_paged_append(d, &s, turn ? &rope : nullptr, kp, ks, vp, vs, tokens, status, reinterpret_cast<void*>(stream));
+        Py_END_ALLOW_THREADS
+      }
+    }
+  } catch (...) { r = kNotPlain; }
+  return PyLong_FromLongLong(r);
+}
+
+// paged_attn(desc address, q, page_table, lengths, n_new, cos, sin, positions, interleaved, out, scale, window, flags, lse, workspace, status, stream)
+// -> status, or the bytes of workspace the call needs and did not bring, or kNotPlain
+PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  long long desc, window, flags, stream, r = kNotPlain;
+  try {
+    if (n == 17 && g_paged_attn && integer(a[0], &desc) && PyFloat_CheckExact(a[10]) && integer(a[11], &window) && integer(a[12], &flags) && integer(a[16], &stream)) {
+      const kvq_paged_cache* d = reinterpret_cast<const kvq_paged_cache*>(desc);
+      const at::Tensor *q = plain(a[1]), *out = plain(a[9]), *lse = a[13] == Py_None ? nullptr : cuda_tensor(a[13], at::kFloat, 3);
+      kvq_paged_batch s;
+      kvq_rope rope;
+      bool turn;
+      int32_t* status;
+      if (q && out && q->sizes() == out->sizes() && q->size(3) == d->head_dim && paged_batch(a + 2, q->size(0), &s) &&
+          paged_rope(a + 5, q->size(0), q->size(2), &rope, &turn) && paged_status(a[15], &status) && q->size(1) <= 0x7FFFFFFF &&
+          (a[13] == Py_None || (lse && lse->is_contiguous() && lse->sizes() == q->sizes().slice(0, 3))) && (a[14] == Py_None || THPVariable_CheckExact(a[14]))) {
+        const int32_t heads = (int32_t)q->size(1);
+        const int64_t m = q->size(2);
+        size_t need = 0, have = 0;
+        r = g_paged_workspace_bytes(d, &s, heads, m, (uint32_t)flags, &need);
+        if (r == KVQ_OK) {
+          void* ws = nullptr;
+          if (need && a[14] != Py_None) {
+            const at::Tensor& w = THPVariable_Unpack(a[14]);
+            have = (size_t)w.numel();
+            if (have >= need) ws = w.data_ptr();
+          }
+          if (need && !ws) {
+            r = (long long)need;
+          } else {
+            const void* qp = q->data_ptr();
+            void *op = out->data_ptr(), *lp = lse ? lse->data_ptr() : nullptr;
+            const kvq_strides qs = paged_strides(*q), os = paged_strides(*out);
+            const float scale = (float)PyFloat_AS_DOUBLE(a[10]);
+            Py_BEGIN_ALLOW_THREADS
+            r = g_paged_attn(d, &s, turn ? &rope : nullptr, qp, qs, heads, m, op, os, scale, window, (uint32_t)flags, static_cast<float*>(lp), ws, have, status,
+                             reinterpret_cast<void*>(stream));
+            Py_END_ALLOW_THREADS
+          }
+        }
+      }
+    }
+  } catch (...) { r = kNotPlain; }
+  return PyLong_FromLongLong(r);
+}
+
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&bind)), METH_FASTCALL, nullptr},
     {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&append)), METH_FASTCALL, nullptr},
     {"attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&attn)), METH_FASTCALL, nullptr},
+    {"bind_paged", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&bind_paged)), METH_FASTCALL, nullptr},
+    {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&paged_append)), METH_FASTCALL, nullptr},
+    {"paged_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&paged_attn)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_py_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
