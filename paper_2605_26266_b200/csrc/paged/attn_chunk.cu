@@ -231,7 +231,10 @@ __global__ void __launch_bounds__(kQueryThreads) paged_query_kernel(const ChunkP
     }
   }
   if ((long long)((int)blockIdx.x - 1) * kTokens * p.group >= used) return;
-  const int64_t at = p.rope.dim ? (int64_t)rope_row(p.rope, b, real ? t : 0, ex.before, real ? p.status : nullptr) * (p.rope.dim >> 1) : 0;
+  bool far = false;
+  Turn turn = {};
+  if (p.rope.dim && real) turn = load_turn(p.rope, rope_row(p.rope, b, t, ex.before, &far), j);
+  if (far) report(p.status, kBadPosition);
   const uint16_t* q = p.q + (int64_t)b * p.qs.b + (int64_t)h * p.group * p.qs.h + (int64_t)t * p.qs.t + 8 * j;
   const int64_t unit0 = ((int64_t)b * p.pool.kv_heads + h) * p.max_blocks;
   for (int g0 = 0; g0 < p.group; g0 += kBatch) {
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(kQueryThreads) paged_query_kernel(const ChunkP
       if (g0 + i >= p.group) break;
       float x[8];
       bf16x8_to_f32(raw[i], x);
-      if (p.rope.dim) rotate8(x, p.rope.cos + at, p.rope.sin + at, p.rope, j);
+      if (p.rope.dim) rotate8(x, turn, p.rope, j);
       const QueryParts<2> qp = query_parts<D, 2, 1>(x);
       const long long row = (long long)t * p.group + g0 + i;
       if (row < used) {

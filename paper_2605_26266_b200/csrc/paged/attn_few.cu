@@ -52,21 +52,21 @@ struct Few {
   static constexpr int kOffP = kOffQ + (kN * D + 1023) / 1024 * 1024;
   static constexpr int kPBytes = kTileKeys * kNP;
   static constexpr int kOffBar = kOffP + 2 * kPBytes;
-  enum { kFull = 0, kEmpty = kFull + kStages, kQFull = kEmpty + kStages, kSFull, kSFree = kSFull + 2, kPFull = kSFree + 2, kPDone = kPFull + 2,
+  enum { kFull = 0, kEmpty = kFull + kStages, kQFull = kEmpty + kStages, kQFree, kSFull, kSFree = kSFull + 2, kPFull = kSFree + 2, kPDone = kPFull + 2,
          kDrain = kPDone + 2, kBars };
   static constexpr int kOffMisc = kOffBar + kBars * 8;              // tmem base, abort
   static constexpr int kOffScale = (kOffMisc + 8 + 15) / 16 * 16;   // [stages][2][8] scale bytes of a tile's pages
-  static constexpr int kOffRow = kOffScale + kStages * 16;          // floats: row factors, 5 - m, f, partial maxima and sums [4][NR]
-  static constexpr int kOffAcc = kOffRow + (3 + 4) * NR * 4;        // whether the product of a buffer adds to O^T
+  static constexpr int kOffRow = kOffScale + kStages * 16;          // floats: row factors of two segments, 5 - m, f, partial maxima and sums [4][NR]
+  static constexpr int kOffAcc = kOffRow + (4 + 4) * NR * 4;        // whether the product of a buffer adds to O^T
   static constexpr int kOffWalk = (kOffAcc + 8 + 15) / 16 * 16;
-  static constexpr int kSmem = kOffWalk + 32 + 1024;
+  static constexpr int kSmem = kOffWalk + 48 + 1024;
   static constexpr int kTmemS = 0, kTmemO = 2 * kN;
   static constexpr int kTmemCols = 2 * kN + kNP <= 128 ? 128 : 256;
   static constexpr int kSlotBytes = NR * (D + 2) * 4;
 };
 
-// A CTA's place in the line of tiles.
-struct Place { int b, h, t; long long left; };
+// A CTA's place in the line of tiles, and what is known of the sequence there.
+struct Place { int b, h, t; Extent ex; Tiles tl; long long left; };
 struct Segment { int b, h, tb, te, n, first; Extent ex; };      // tiles [tb, te) of the unit's n, which begin with tile `first` of the sequence
 
 struct Walker {
@@ -74,7 +74,7 @@ struct Walker {
   Extent ex;
   Tiles tl;
   bool known;
-  __device__ __forceinline__ Walker(const Place& p) : at(p), known(false) {}
+  __device__ __forceinline__ Walker(const Place& p) : at(p), ex(p.ex), tl(p.tl), known(true) {}
   __device__ __forceinline__ bool next(Segment& s, const FewParams& p) {
     if (at.left <= 0) return false;
     while (!known) {
@@ -92,24 +92,24 @@ struct Walker {
   }
 };
 
-// One warp: the place of CTA c of n in the line.
+// One warp: the place of CTA c of n in the line.  Lengths are read once where a lane has one sequence at most.
 __device__ __forceinline__ Place find_place(const FewParams& p, int c, int n) {
   const int lane = threadIdx.x & 31;
-  auto tiles_at = [&](int b) -> long long {
-    if (b >= p.seqs.batch) return 0;
-    const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, p.status);
-    return (long long)tiles_of(ex, 0, p.m_tokens, p.causal, p.window).count * p.pool.kv_heads;
-  };
-  long long all = 0;
-  for (int b = lane; b < p.seqs.batch; b += 32) all += tiles_at(b);
+  auto extent_at = [&](int b, int32_t* status) { return b < p.seqs.batch ? extent_of(p.seqs, p.pool.page, b, p.m_tokens, status) : Extent{0, 0}; };
+  auto tiles_at = [&](const Extent& ex) { return (long long)tiles_of(ex, 0, p.m_tokens, p.causal, p.window).count * p.pool.kv_heads; };
+  const Extent ex0 = extent_at(lane, p.status);
+  long long all = tiles_at(ex0);
+  for (int b = lane + 32; b < p.seqs.batch; b += 32) all += tiles_at(extent_at(b, p.status));
   for (int i = 16; i; i >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, i);
   n = (int)min((long long)n, all);                       // so that no range between two others is empty
-  if (c >= n) return Place{0, 0, 0, 0};
+  Place r{};
+  if (c >= n) return r;
   const long long lo = all * c / n, hi = all * (c + 1) / n;
-  Place r{0, 0, 0, hi - lo};
+  r.left = hi - lo;
   long long before = 0;
   for (int b0 = 0;; b0 += 32) {
-    const long long mine = tiles_at(b0 + lane);
+    const Extent ex = b0 ? extent_at(b0 + lane, nullptr) : ex0;
+    const long long mine = tiles_at(ex);
     long long upto = mine;
     for (int i = 1; i < 32; i <<= 1) {
       const long long o = __shfl_up_sync(0xFFFFFFFFu, upto, i);
@@ -121,6 +121,8 @@ __device__ __forceinline__ Place find_place(const FewParams& p, int c, int n) {
       const long long in = lo - before - __shfl_sync(0xFFFFFFFFu, upto - mine, src);
       const int per = (int)(__shfl_sync(0xFFFFFFFFu, mine, src) / p.pool.kv_heads);
       r.b = b0 + src; r.h = (int)(in / per); r.t = (int)(in % per);
+      r.ex = Extent{__shfl_sync(0xFFFFFFFFu, ex.before, src), __shfl_sync(0xFFFFFFFFu, ex.fresh, src)};
+      r.tl = tiles_of(r.ex, 0, p.m_tokens, p.causal, p.window);
       return r;
     }
     before += __shfl_sync(0xFFFFFFFFu, upto, 31);
@@ -164,7 +166,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   if (tid == 0) {
     misc[1] = 0;
     for (int s = 0; s < F::kStages; ++s) { mbar_init(cx.bar(F::kFull + s), 1); mbar_init(cx.bar(F::kEmpty + s), 1); }
-    mbar_init(cx.bar(F::kQFull), 128);
+    mbar_init(cx.bar(F::kQFull), 64); mbar_init(cx.bar(F::kQFree), 1);
     mbar_init(cx.bar(F::kDrain), 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(cx.bar(F::kSFull + s), 1); mbar_init(cx.bar(F::kSFree + s), 128);
@@ -265,7 +267,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     int it = 0, nseg = 0;
     bool ok = true;
     auto all = [](bool x) -> bool { return __all_sync(0xFFFFFFFFu, x); };      // the warp stays together, also on its way out
-    auto scores = [&](int i) {
+    auto scores = [&](int i, bool last) {
       const int s = i % F::kStages, buf = i & 1;
       if (!all(cx.wait(F::kFull + s, i / F::kStages & 1, 611)) || !all(cx.wait(F::kSFree + buf, (i >> 1 & 1) ^ 1, 612))) return false;
       tc_fence_after();
@@ -274,15 +276,17 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         for (int k = 0; k < D / 32; ++k)
           mma_e4m3_ss(tmem + F::kTmemS + buf * F::kN, dk + (uint64_t)((s * 2 * F::kTile + 32 * k) >> 4), dq + (uint64_t)(2 * k), idesc_s, k > 0);
         tc_commit(cx.bar(F::kSFull + buf));
+        if (last) tc_commit(cx.bar(F::kQFree));
       }
+      __syncwarp();
       return true;
     };
     while (ok && w.next(sg, p)) {
       if (!(ok = all(cx.wait(F::kQFull, nseg & 1, 613)))) break;
       tc_fence_after();
-      if (!(ok = scores(it))) break;
+      if (!(ok = scores(it, sg.te - sg.tb == 1))) break;
       for (int t = sg.tb; t < sg.te; ++t, ++it) {
-        if (t + 1 < sg.te && !(ok = scores(it + 1))) break;
+        if (t + 1 < sg.te && !(ok = scores(it + 1, t + 2 == sg.te))) break;
         const int s = it % F::kStages, buf = it & 1;
         if (!(ok = all(cx.wait(F::kPFull + buf, it >> 1 & 1, 614)))) break;
         tc_fence_after();
@@ -306,8 +310,53 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     if (ok) {
       for (int k = max(it - F::kStages, 0); k < it; ++k) cx.drain(F::kEmpty + k % F::kStages, k / F::kStages & 1);
       for (int k = max(it - 2, 0); k < it; ++k) cx.drain(F::kPDone + (k & 1), k >> 1 & 1);
+      if (nseg > 0) cx.drain(F::kQFree, (nseg - 1) & 1);
     }
   } else if (warp < 4) {
+    // ================= the queries of a segment, while the one before is still worked on =================
+    {
+      Walker w(place);
+      Segment sg;
+      int nseg = 0;
+      bool far = false;
+      const int id = tid - 64, j = id % (D / 8), rows = p.group * p.m_tokens;
+      constexpr int kAtOnce = 64 / (D / 8), kPasses = NR / kAtOnce > 0 ? NR / kAtOnce : 1, kBatch = kPasses < 4 ? kPasses : 4;
+      while (w.next(sg, p)) {
+        if (nseg > 0 && !__all_sync(0xFFFFFFFFu, cx.wait(F::kQFree, (nseg - 1) & 1, 631))) break;
+        float* rowf = reinterpret_cast<float*>(smem + F::kOffRow) + (nseg & 1) * NR;
+#pragma unroll 1
+        for (int p0 = 0; p0 < kPasses; p0 += kBatch) {
+          uint4 raw[kBatch];
+          Turn turn[kBatch];
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int r = (p0 + i) * kAtOnce + id / (D / 8), t = r / p.group, g = r - t * p.group;
+            raw[i] = make_uint4(0, 0, 0, 0);
+            if (r < rows && t < sg.ex.fresh) {
+              raw[i] = *reinterpret_cast<const uint4*>(p.q + (int64_t)sg.b * p.qs.b + (int64_t)(sg.h * p.group + g) * p.qs.h + (int64_t)t * p.qs.t + 8 * j);
+              if (p.rope.dim) turn[i] = load_turn(p.rope, rope_row(p.rope, sg.b, t, sg.ex.before, &far), j);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int r = (p0 + i) * kAtOnce + id / (D / 8);
+            float x[8];
+            bf16x8_to_f32(raw[i], x);
+            if (p.rope.dim) rotate8(x, turn[i], p.rope, j);
+            const QueryParts<3> qp = query_parts<D, 3>(x);
+            if (r < NR) {
+#pragma unroll
+              for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(smem + F::kOffQ + RowLayout<D>::at(k * NR + r, 8 * j)) = qp.part[k];
+              if (j == 0) rowf[r] = qp.factor * p.scale_log2;
+            }
+          }
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(cx.bar(F::kQFull));
+        ++nseg;
+      }
+      if (far) report(p.status, kBadPosition);
+    }
     // ================= rows that see nothing =================
     for (int b = blockIdx.x; b < p.seqs.batch; b += gridDim.x) {
       const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, nullptr);
@@ -323,8 +372,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     // ================= softmax: a key of the tile a thread =================
     const int key = tid - 128, wq = warp & 3;
     const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
-    float* rowf = reinterpret_cast<float*>(smem + F::kOffRow);      // factor of a row's scores
-    float* shift = rowf + NR;                                       // 5 - m
+    const float* rowfs = reinterpret_cast<const float*>(smem + F::kOffRow);      // factors of the rows' scores, of two segments
+    float* shift = reinterpret_cast<float*>(smem + F::kOffRow) + 2 * NR;         // 5 - m
     float* drop = shift + NR;                                       // 2^(old m - new m)
     float* part = drop + NR;                                        // [4][NR]
     volatile int* accumulate = reinterpret_cast<volatile int*>(smem + F::kOffAcc);
@@ -336,29 +385,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     int it = 0, nseg = 0;
     bool ok = true;
     while (ok && w.next(sg, p)) {
-      // ---- the rows of this unit, in parts ----
       const int total = sg.ex.before + sg.ex.fresh;
-#pragma unroll 1
-      for (int r0 = 0; r0 < NR; r0 += 128 / (D / 8)) {
-        const int r = r0 + key / (D / 8), j = key % (D / 8);
-        const int t = r / p.group, g = r - t * p.group;
-        const bool real = r < NR && t < sg.ex.fresh && r < rows;
-        float x[8] = {};
-        if (real)
-          bf16x8_to_f32(*reinterpret_cast<const uint4*>(p.q + (int64_t)sg.b * p.qs.b + (int64_t)(sg.h * p.group + g) * p.qs.h + (int64_t)t * p.qs.t + 8 * j), x);
-        if (p.rope.dim) {
-          const int64_t at = (int64_t)rope_row(p.rope, sg.b, real ? t : 0, sg.ex.before, real ? p.status : nullptr) * (p.rope.dim >> 1);
-          rotate8(x, p.rope.cos + at, p.rope.sin + at, p.rope, j);
-        }
-        const QueryParts<3> qp = query_parts<D, 3>(x);
-        if (r < NR) {
-#pragma unroll
-          for (int i = 0; i < 3; ++i) *reinterpret_cast<uint2*>(smem + F::kOffQ + RowLayout<D>::at(i * NR + r, 8 * j)) = qp.part[i];
-          if (j == 0) { rowf[r] = qp.factor * p.scale_log2; shift[r] = kBase + 1e30f; }
-        }
-      }
-      fence_proxy_async_smem();
-      mbar_arrive(cx.bar(F::kQFull));
+      const float* rowf = rowfs + (nseg & 1) * NR;
+      if (key < NR) shift[key] = kBase + 1e30f;
       named_barrier_sync(1, 128);
       float l[NR], o[NR];
 #pragma unroll
@@ -484,19 +513,21 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       const int slot = nseg == 0 ? 0 : 1;
       float* to = whole ? nullptr : reinterpret_cast<float*>(p.slots + (size_t)(2 * blockIdx.x + slot) * F::kSlotBytes);
       if (!whole && key == 0) header[slot] = make_int4(sg.tb == 0 ? kStart : sg.te == sg.n ? kEnd : kMiddle, sg.b, sg.h, sg.ex.fresh);
+      uint16_t* out = p.out + (int64_t)sg.b * p.os.b + (int64_t)sg.h * p.group * p.os.h + key;
+      float* lse = p.lse ? p.lse + ((int64_t)sg.b * p.q_heads + sg.h * p.group) * p.m_tokens : nullptr;
+      int t = 0, g = 0;                                             // of row r
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
-        const int t = r / p.group, g = r - t * p.group;
-        if (r >= rows || t >= sg.ex.fresh) continue;
+        if (r >= rows || t >= sg.ex.fresh) break;
         const float sum = part[r] + part[NR + r] + part[2 * NR + r] + part[3 * NR + r];
         if (whole) {
-          const int h = sg.h * p.group + g;
-          if (key < D) p.out[(int64_t)sg.b * p.os.b + (int64_t)h * p.os.h + (int64_t)t * p.os.t + key] = (uint16_t)f32_to_bf16_bits(sum == 0.f ? 0.f : o[r] / sum);
-          if (p.lse && key == 0) p.lse[((int64_t)sg.b * p.q_heads + h) * p.m_tokens + t] = (log2f(sum) - shift[r]) * 0.6931471805599453f;
+          if (key < D) out[(int64_t)g * p.os.h + (int64_t)t * p.os.t] = (uint16_t)f32_to_bf16_bits(sum == 0.f ? 0.f : __fdividef(o[r], sum));
+          if (lse && key == 0) lse[(int64_t)g * p.m_tokens + t] = (log2f(sum) - shift[r]) * 0.6931471805599453f;
         } else {
           if (key < D) to[r * D + key] = o[r];
           if (key == 0) { to[NR * D + r] = -shift[r]; to[NR * D + NR + r] = sum; }
         }
+        if (++g == p.group) { g = 0; ++t; }
       }
       named_barrier_sync(1, 128);                                   // shift and part are the next segment's now
       ++nseg;
@@ -524,16 +555,28 @@ __global__ void __launch_bounds__(D) paged_few_merge_kernel(const FewParams p, i
   if (hd.x != kStart) { hd = load_coherent(p.headers + 2 * c + 1); slot = 1; }
   const int t = r / p.group, g = r - t * p.group;
   if (hd.x != kStart || t >= hd.w) return;
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int k = c;; ++k) {
-    const float* from = reinterpret_cast<const float*>(p.slots + (size_t)(2 * k + (k == c ? slot : 0)) * F::kSlotBytes);
-    const float mk = load_coherent(from + NR * D + r), lk = load_coherent(from + NR * D + NR + r), ok = load_coherent(from + r * D + d);
-    const float top = fmaxf(m, mk), a = ex2(m - top), b = ex2(mk - top);
-    l = l * a + lk * b;
-    o = o * a + ok * b;
-    m = top;
-    if (k > c && load_coherent(p.headers + 2 * k).x != kMiddle) break;
-    if (k + 1 == ctas) break;
+  // the last CTA that worked on the unit, and the largest of the maxima: 32 parts at a time
+  const int lane = d & 31;
+  auto slot_of = [&](int k) { return reinterpret_cast<const float*>(p.slots + (size_t)(2 * k + (k == c ? slot : 0)) * F::kSlotBytes); };
+  int end = ctas;
+  float m = -INFINITY;
+  for (int k0 = c; k0 < end; k0 += 32) {
+    const int k = k0 + lane;
+    const bool last = k > c && k < ctas && load_coherent(p.headers + 2 * k).x != kMiddle;
+    float mk = k < ctas ? load_coherent(slot_of(k) + NR * D + r) : -INFINITY;
+    const unsigned ends = __ballot_sync(0xFFFFFFFFu, last);
+    if (ends) end = k0 + __ffs(ends);
+    if (k >= end) mk = -INFINITY;
+    for (int i = 16; i; i >>= 1) mk = fmaxf(mk, __shfl_xor_sync(0xFFFFFFFFu, mk, i));
+    m = fmaxf(m, mk);
+  }
+  float l = 0.f, o = 0.f;
+#pragma unroll 8
+  for (int k = c; k < end; ++k) {
+    const float* from = slot_of(k);
+    const float a = ex2(load_coherent(from + NR * D + r) - m);
+    l = fmaf(load_coherent(from + NR * D + NR + r), a, l);
+    o = fmaf(load_coherent(from + r * D + d), a, o);
   }
   const int h = hd.z * p.group + g;
   p.out[(int64_t)hd.y * p.os.b + (int64_t)h * p.os.h + (int64_t)t * p.os.t + d] = (uint16_t)f32_to_bf16_bits(l == 0.f ? 0.f : o / l);

@@ -100,53 +100,57 @@ __device__ __forceinline__ Tiles tiles_of(const Extent& ex, int t0, int t1, bool
   return {first, (end + kTileKeys - 1) / kTileKeys - first};
 }
 
-// Row of the rotation's tables for new token t of sequence b.
-__device__ __forceinline__ int rope_row(const Rope& r, int b, int t, int before, int32_t* status) {
-  int row = r.positions ? load_coherent(r.positions + (int64_t)b * r.positions_stride + t) : before + t;
-  if (row < 0 || row >= r.rows) {
-    report(status, kBadPosition);
-    row = row < 0 ? 0 : r.rows - 1;
-  }
-  return row;
+// Row of the rotation's tables for new token t of sequence b; the nearest one, and *bad set, where they have no such row.
+__device__ __forceinline__ int rope_row(const Rope& r, int b, int t, int before, bool* bad) {
+  const int row = r.positions ? load_coherent(r.positions + (int64_t)b * r.positions_stride + t) : before + t;
+  const int in = min(max(row, 0), r.rows - 1);
+  *bad |= in != row;
+  return in;
 }
 
-// Rotates the 8 channels [8 j, 8 j + 8) that this lane holds of a row of D channels spread over D / 8 neighbouring lanes (all of
-// them here).  cs, sn: the row of the tables.  Every product and sum is rounded by itself, so that the result is that of the
-// formulas in binary32, whoever computes them.  Pairs lie side by side (interleaved), or dim / 2 channels apart, in another lane.
-__device__ __forceinline__ void rotate8(float (&x)[8], const float* cs, const float* sn, const Rope& r, int j) {
+// Rotation of a row of D channels spread over D / 8 neighbouring lanes, 8 channels [8 j, 8 j + 8) each.  Pairs lie side by side (interleaved), or dim / 2
+// channels apart, in another lane.  What a lane needs of the tables' row comes first, so that several rows' can be on their way.
+struct Turn { float c[8], s[8]; };
+__device__ __forceinline__ Turn load_turn(const Rope& r, int row, int j) {
+  Turn t;
+  const int chunks = r.dim >> 3, half = chunks >> 1;
+  if (j < chunks) {
+    const int64_t at = (int64_t)row * (r.dim >> 1) + (r.interleaved ? 4 * j : 8 * (j < half ? j : j - half));
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      if (i && r.interleaved) break;
+      const float4 c = *reinterpret_cast<const float4*>(r.cos + at + i), s = *reinterpret_cast<const float4*>(r.sin + at + i);
+      t.c[i] = c.x; t.c[i + 1] = c.y; t.c[i + 2] = c.z; t.c[i + 3] = c.w;
+      t.s[i] = s.x; t.s[i + 1] = s.y; t.s[i + 2] = s.z; t.s[i + 3] = s.w;
+    }
+  }
+  return t;
+}
+// All lanes of the warp are here.  Every product and sum is rounded by itself.
+__device__ __forceinline__ void rotate8(float (&x)[8], const Turn& t, const Rope& r, int j) {
   const int chunks = r.dim >> 3;
   if (r.interleaved) {
     if (j < chunks) {
-      const float4 c = *reinterpret_cast<const float4*>(cs + 4 * j), s = *reinterpret_cast<const float4*>(sn + 4 * j);
-      const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float a = x[2 * i], b = x[2 * i + 1];
-        x[2 * i] = __fsub_rn(__fmul_rn(a, cc[i]), __fmul_rn(b, ss[i]));
-        x[2 * i + 1] = __fadd_rn(__fmul_rn(b, cc[i]), __fmul_rn(a, ss[i]));
+        x[2 * i] = __fsub_rn(__fmul_rn(a, t.c[i]), __fmul_rn(b, t.s[i]));
+        x[2 * i + 1] = __fadd_rn(__fmul_rn(b, t.c[i]), __fmul_rn(a, t.s[i]));
       }
     }
     return;
   }
-  const int half = chunks >> 1;
-  const int lane = threadIdx.x & 31;
+  const int half = chunks >> 1, lane = threadIdx.x & 31;
   const bool low = j < half, in = j < chunks;
   const int from = in ? (low ? lane + half : lane - half) : lane;
   float y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xFFFFFFFFu, x[i], from);
   if (in) {
-    const int at = 8 * (low ? j : j - half);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float4 c = *reinterpret_cast<const float4*>(cs + at + 4 * h), s = *reinterpret_cast<const float4*>(sn + at + 4 * h);
-      const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float& v = x[4 * h + i];
-        const float mine = __fmul_rn(v, cc[i]), other = __fmul_rn(y[4 * h + i], ss[i]);
-        v = low ? __fsub_rn(mine, other) : __fadd_rn(mine, other);
-      }
+    for (int i = 0; i < 8; ++i) {
+      const float mine = __fmul_rn(x[i], t.c[i]), other = __fmul_rn(y[i], t.s[i]);
+      x[i] = low ? __fsub_rn(mine, other) : __fadd_rn(mine, other);
     }
   }
 }
