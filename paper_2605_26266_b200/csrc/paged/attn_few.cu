@@ -47,11 +47,13 @@ struct Few {
   static constexpr int kN = NR == 8 ? 32 : 3 * NR;                  // columns of S^T: three parts (a multiple of 16)
   static constexpr int kNP = 2 * NR;                                // columns of O^T
   static constexpr int kTile = kTileKeys * D;                       // bytes of a tile of keys or values
-  static constexpr int kStages = D == 128 ? 6 : 8;
+  static constexpr int kStages = D == 64 ? 8 : NR == 32 ? 5 : 6;
   static constexpr int kOffQ = kStages * 2 * kTile;
   static constexpr int kOffP = kOffQ + (kN * D + 1023) / 1024 * 1024;
   static constexpr int kPBytes = kTileKeys * kNP;
-  static constexpr int kOffBar = kOffP + 2 * kPBytes;
+  static constexpr int kOffRaw = kOffP + 2 * kPBytes;              // queries of a unit as they come, and their rows of the rotation's tables
+  static constexpr int kRawRow = 2 * D + 4 * D;
+  static constexpr int kOffBar = kOffRaw + NR * kRawRow;
   enum { kFull = 0, kEmpty = kFull + kStages, kQFull = kEmpty + kStages, kQFree, kSFull, kSFree = kSFull + 2, kPFull = kSFree + 2, kPDone = kPFull + 2,
          kDrain = kPDone + 2, kBars };
   static constexpr int kOffMisc = kOffBar + kBars * 8;              // tmem base, abort
@@ -104,7 +106,8 @@ __device__ __forceinline__ Place find_place(const FewParams& p, int c, int n) {
   n = (int)min((long long)n, all);                       // so that no range between two others is empty
   Place r{};
   if (c >= n) return r;
-  const long long lo = all * c / n, hi = all * (c + 1) / n;
+  auto cut = [&](int i) { return all < 1 << 22 ? (long long)((uint32_t)all * (uint32_t)i / (uint32_t)n) : all * i / n; };      // at most 1024 CTAs
+  const long long lo = cut(c), hi = cut(c + 1);
   r.left = hi - lo;
   long long before = 0;
   for (int b0 = 0;; b0 += 32) {
@@ -119,10 +122,12 @@ __device__ __forceinline__ Place find_place(const FewParams& p, int c, int n) {
     if (hit) {
       const int src = __ffs(hit) - 1;
       const long long in = lo - before - __shfl_sync(0xFFFFFFFFu, upto - mine, src);
-      const int per = (int)(__shfl_sync(0xFFFFFFFFu, mine, src) / p.pool.kv_heads);
-      r.b = b0 + src; r.h = (int)(in / per); r.t = (int)(in % per);
       r.ex = Extent{__shfl_sync(0xFFFFFFFFu, ex.before, src), __shfl_sync(0xFFFFFFFFu, ex.fresh, src)};
       r.tl = tiles_of(r.ex, 0, p.m_tokens, p.causal, p.window);
+      const int per = r.tl.count;
+      r.b = b0 + src;
+      if (in < 1 << 30) { r.h = (int)in / per; r.t = (int)in % per; }
+      else { r.h = (int)(in / per); r.t = (int)(in % per); }
       return r;
     }
     before += __shfl_sync(0xFFFFFFFFu, upto, 31);
@@ -145,6 +150,11 @@ __device__ __forceinline__ bool barrier_or(uint32_t id, uint32_t n, bool x) {
                : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)x) : "memory");
   return r != 0;
 }
+// 16 bytes from global to shared memory, on their way until copies_done().
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r) {
 #pragma unroll
@@ -320,35 +330,49 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       int nseg = 0;
       bool far = false;
       const int id = tid - 64, j = id % (D / 8), rows = p.group * p.m_tokens;
-      constexpr int kAtOnce = 64 / (D / 8), kPasses = NR / kAtOnce > 0 ? NR / kAtOnce : 1, kBatch = kPasses < 4 ? kPasses : 4;
+      constexpr int kAtOnce = 64 / (D / 8), kPasses = NR / kAtOnce > 0 ? NR / kAtOnce : 1;      // rows at a time
       while (w.next(sg, p)) {
         if (nseg > 0 && !__all_sync(0xFFFFFFFFu, cx.wait(F::kQFree, (nseg - 1) & 1, 631))) break;
         float* rowf = reinterpret_cast<float*>(smem + F::kOffRow) + (nseg & 1) * NR;
+        // All that the rows need is on its way at once: with the tiles streaming, a load takes up to 5 000 cycles, and one row after the other held up the
+        // first unit for longer than its first five tiles.  Rolled loops: their code is new to the SM as well.
+        auto raw_of = [&](int r) { return smem + F::kOffRaw + r * F::kRawRow; };
 #pragma unroll 1
-        for (int p0 = 0; p0 < kPasses; p0 += kBatch) {
-          uint4 raw[kBatch];
-          Turn turn[kBatch];
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int r = (p0 + i) * kAtOnce + id / (D / 8), t = r / p.group, g = r - t * p.group;
-            raw[i] = make_uint4(0, 0, 0, 0);
-            if (r < rows && t < sg.ex.fresh) {
-              raw[i] = *reinterpret_cast<const uint4*>(p.q + (int64_t)sg.b * p.qs.b + (int64_t)(sg.h * p.group + g) * p.qs.h + (int64_t)t * p.qs.t + 8 * j);
-              if (p.rope.dim) turn[i] = load_turn(p.rope, rope_row(p.rope, sg.b, t, sg.ex.before, &far), j);
+        for (int pass = 0; pass < kPasses; ++pass) {
+          const int r = pass * kAtOnce + id / (D / 8), t = r / p.group, g = r - t * p.group;
+          if (r >= NR) break;
+          const uint32_t to = smem_u32(raw_of(r));
+          if (r < rows && t < sg.ex.fresh) {
+            copy16(to + 16 * j, p.q + (int64_t)sg.b * p.qs.b + (int64_t)(sg.h * p.group + g) * p.qs.h + (int64_t)t * p.qs.t + 8 * j);
+            if (8 * j < p.rope.dim) {
+              const int64_t at = (int64_t)rope_row(p.rope, sg.b, t, sg.ex.before, &far) * (p.rope.dim >> 1) + 4 * j;
+              copy16(to + 2 * D + 16 * j, p.rope.cos + at);
+              copy16(to + 4 * D + 16 * j, p.rope.sin + at);
             }
+          } else {
+            *reinterpret_cast<uint4*>(raw_of(r) + 16 * j) = make_uint4(0, 0, 0, 0);
           }
+        }
+        copies_done();
+        __syncwarp();                                              // a row's lanes are one warp's
+#pragma unroll 1
+        for (int pass = 0; pass < kPasses; ++pass) {
+          const int r = pass * kAtOnce + id / (D / 8);
+          float x[8] = {};
+          Turn now = {};
+          if (r < NR) {
+            bf16x8_to_f32(*reinterpret_cast<const uint4*>(raw_of(r) + 16 * j), x);
+            Rope here = p.rope;
+            here.cos = reinterpret_cast<const float*>(raw_of(r) + 2 * D);
+            here.sin = reinterpret_cast<const float*>(raw_of(r) + 4 * D);
+            if (p.rope.dim) now = load_turn(here, 0, j);
+          }
+          if (p.rope.dim) rotate8(x, now, p.rope, j);
+          const QueryParts<3> qp = query_parts<D, 3>(x);
+          if (r < NR) {
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int r = (p0 + i) * kAtOnce + id / (D / 8);
-            float x[8];
-            bf16x8_to_f32(raw[i], x);
-            if (p.rope.dim) rotate8(x, turn[i], p.rope, j);
-            const QueryParts<3> qp = query_parts<D, 3>(x);
-            if (r < NR) {
-#pragma unroll
-              for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(smem + F::kOffQ + RowLayout<D>::at(k * NR + r, 8 * j)) = qp.part[k];
-              if (j == 0) rowf[r] = qp.factor * p.scale_log2;
-            }
+            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(smem + F::kOffQ + RowLayout<D>::at(k * NR + r, 8 * j)) = qp.part[k];
+            if (j == 0) rowf[r] = qp.factor * p.scale_log2;
           }
         }
         fence_proxy_async_smem();
@@ -493,13 +517,26 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
       // ---- the rows' sums: l over the 128 keys of a thread each, O^T from TMEM, a channel a thread ----
       ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + ((it - 1) & 1), (it - 1) >> 1 & 1, 625));
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
-#pragma unroll
-        for (int i = 16; i; i >>= 1) l[r] += __shfl_xor_sync(0xFFFFFFFFu, l[r], i);
-        if (lane == 0) part[wq * NR + r] = l[r];
-      }
       if (barrier_or(1, 128, !ok)) { ok = false; break; }
+      {
+        // over the buffers of the weights, whose last product is done
+        float* sums = reinterpret_cast<float*>(smem + F::kOffP);
+        constexpr int kPer = 128 / NR;                              // threads of a row
+#pragma unroll
+        for (int r = 0; r < NR; ++r) sums[r * 128 + key] = l[r];
+        named_barrier_sync(1, 128);
+        const float4* mine = reinterpret_cast<const float4*>(sums + key / kPer * 128) + key % kPer;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < NR / 4; ++i) {
+          const float4 x = mine[i * kPer];
+          sum += (x.x + x.y) + (x.z + x.w);
+        }
+#pragma unroll
+        for (int i = kPer / 2; i; i >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
+        if (key % kPer == 0) part[key / kPer] = sum;
+        named_barrier_sync(1, 128);
+      }
       tc_fence_after();
       {
         uint32_t raw[F::kNP];
@@ -519,7 +556,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 #pragma unroll
       for (int r = 0; r < NR; ++r) {
         if (r >= rows || t >= sg.ex.fresh) break;
-        const float sum = part[r] + part[NR + r] + part[2 * NR + r] + part[3 * NR + r];
+        const float sum = part[r];
         if (whole) {
           if (key < D) out[(int64_t)g * p.os.h + (int64_t)t * p.os.t] = (uint16_t)f32_to_bf16_bits(sum == 0.f ? 0.f : __fdividef(o[r], sum));
           if (lse && key == 0) lse[(int64_t)g * p.m_tokens + t] = (log2f(sum) - shift[r]) * 0.6931471805599453f;
