@@ -41,18 +41,6 @@ __device__ __forceinline__ int exponent_of(uint32_t bits) {
 // memory 29.3; 256 threads an SM 33.7.
 __host__ __device__ constexpr int threads_of(int d, int page) { return page * d / 64 < 32 ? 32 : page * d / 64; }
 
-// 16 channels of a token that a lane has: two chunks of 8.  x[0..7] and x[8..15] are partners of the rotation, number by number: chunks that lie dim / 2
-// channels apart, or the even and the odd channels of two neighbouring chunks.
-template <bool INTERLEAVED>
-__device__ __forceinline__ void unpack(const uint4& a, const uint4& b, float (&x)[16]) {
-  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xFFFF0000u);
-    if (INTERLEAVED) { x[i] = lo; x[8 + i] = hi; }
-    else { x[2 * i] = lo; x[2 * i + 1] = hi; }
-  }
-}
 template <bool INTERLEAVED>
 __device__ __forceinline__ void pack(const float (&x)[16], float f, uint2& a, uint2& b) {
   uint32_t w[8];
@@ -64,22 +52,6 @@ __device__ __forceinline__ void pack(const float (&x)[16], float f, uint2& a, ui
   a = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
   b = make_uint2(w[4] | w[5] << 16, w[6] | w[7] << 16);
 }
-// Every product and sum is rounded by itself: the result is that of the formulas in binary32, whoever computes them.  (Packed products and sums of
-// two numbers are made FMAs on the way to the machine, with explicit rounding too: nine codes of 14 million came out differently.)
-__device__ __forceinline__ void rotate16(float (&x)[16], const float* cs, const float* sn) {
-#pragma unroll
-  for (int i = 0; i < 8; i += 4) {
-    const float4 c = *reinterpret_cast<const float4*>(cs + i), s = *reinterpret_cast<const float4*>(sn + i);
-    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const float u = x[i + h], w = x[8 + i + h];
-      x[i + h] = __fsub_rn(__fmul_rn(u, cc[h]), __fmul_rn(w, ss[h]));
-      x[8 + i + h] = __fadd_rn(__fmul_rn(w, cc[h]), __fmul_rn(u, ss[h]));
-    }
-  }
-}
-
 template <int D, int PAGE, bool INTERLEAVED>
 __global__ void __launch_bounds__(threads_of(D, PAGE), 512 / threads_of(D, PAGE)) paged_append_kernel(const AppendParams p) {
   constexpr int kThreads = threads_of(D, PAGE), kLanes = D / 16, kRows = kThreads / kLanes, kPer = PAGE / kRows;      // lanes of a token; tokens at a time; passes
@@ -97,10 +69,9 @@ __global__ void __launch_bounds__(threads_of(D, PAGE), 512 / threads_of(D, PAGE)
   const int lane = tid % kLanes, r0 = tid / kLanes;
   const int64_t tok0 = (int64_t)first * PAGE - ex.before;                      // new token of slot 0
   // this lane's chunks of a key, and the column of the tables that their rotation begins with
-  const int turned = p.rope.dim >> 4;
-  const bool turn = lane < turned;
-  const int ca = INTERLEAVED || !turn ? (INTERLEAVED ? 2 * lane : 2 * turned + 2 * (lane - turned)) : lane;
-  const int cb = INTERLEAVED || !turn ? ca + 1 : lane + turned;
+  const bool turn = lane < p.rope.dim >> 4;
+  const Chunks mine = chunks_of<INTERLEAVED>(lane, p.rope.dim);
+  const int ca = mine.a, cb = mine.b;
   const uint16_t* kp = p.k + (int64_t)b * p.ks.b + (int64_t)h * p.ks.h;
   const uint16_t* vp = p.v + (int64_t)b * p.vs.b + (int64_t)h * p.vs.h + 8 * lane;      // of a value: chunks lane and lane + kLanes
   uint4 ka[kPer], kb[kPer], va[kPer], vb[kPer];

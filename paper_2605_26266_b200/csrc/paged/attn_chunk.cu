@@ -186,6 +186,13 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// tcgen05.wait::ld with the registers of a load that was issued long before: nothing that uses them may come ahead of it.
+__device__ __forceinline__ void tmem_wait_ld_of(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]),"+r"(r[1]),"+r"(r[2]),"+r"(r[3]),"+r"(r[4]),"+r"(r[5]),"+r"(r[6]),"+r"(r[7]),"+r"(r[8]),"+r"(r[9]),"+r"(r[10]),"+r"(r[11]),"+r"(r[12]),"+r"(r[13]),"+r"(r[14]),"+r"(r[15]),"+r"(r[16]),"+r"(r[17]),"+r"(r[18]),"+r"(r[19]),"+r"(r[20]),"+r"(r[21]),"+r"(r[22]),"+r"(r[23]),"+r"(r[24]),"+r"(r[25]),"+r"(r[26]),"+r"(r[27]),"+r"(r[28]),"+r"(r[29]),"+r"(r[30]),"+r"(r[31]) :: "memory");
+}
+__device__ __forceinline__ bool all_lanes(bool x) { return __all_sync(0xFFFFFFFFu, x); }
+
 __device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
@@ -197,68 +204,100 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t w) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(in));
   return h;
 }
-// tcgen05.wait::ld with the registers of a load that was issued long before: nothing that uses them may come ahead of it.
-__device__ __forceinline__ void tmem_wait_ld_of(uint32_t* r) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]),"+r"(r[1]),"+r"(r[2]),"+r"(r[3]),"+r"(r[4]),"+r"(r[5]),"+r"(r[6]),"+r"(r[7]),"+r"(r[8]),"+r"(r[9]),"+r"(r[10]),"+r"(r[11]),"+r"(r[12]),"+r"(r[13]),"+r"(r[14]),"+r"(r[15]),"+r"(r[16]),"+r"(r[17]),"+r"(r[18]),"+r"(r[19]),"+r"(r[20]),"+r"(r[21]),"+r"(r[22]),"+r"(r[23]),"+r"(r[24]),"+r"(r[25]),"+r"(r[26]),"+r"(r[27]),"+r"(r[28]),"+r"(r[29]),"+r"(r[30]),"+r"(r[31]) :: "memory");
+__device__ __forceinline__ uint32_t f16x2_to_e4m3x2(uint32_t h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+  return r;
 }
-__device__ __forceinline__ bool all_lanes(bool x) { return __all_sync(0xFFFFFFFFu, x); }
+__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
 
 // The queries of a call (and its schedule, by one block): rotated, in two E4M3 parts, laid out as the query tiles of the chunk kernel's units are in shared memory, so that one bulk copy
 // brings a tile.  A token's rotation is read once for the query heads of a key head.  (The four expanding warps of the chunk kernel did this between two
 // units; loads and shuffles of 256 rows one after the other held up the unit for longer than the rows take on the whole GPU.)
 constexpr int kQueryThreads = kRows;
-template <int D>
+template <int D, bool INTERLEAVED>
 __global__ void __launch_bounds__(kQueryThreads) paged_query_kernel(const ChunkParams p, int ctas) {
   using F = Chunk<D>;
-  constexpr int kLanes = D / 8, kTokens = kQueryThreads / kLanes, kBatch = 4;
+  constexpr int kLanes = D / 16, kTokens = kQueryThreads / kLanes, kBatch = 4;
   wait_for_previous_grid();
   allow_next_grid();
   if (blockIdx.x == 0) {                                     // ahead of the others: the chunk kernel waits for it too
     if (blockIdx.y == 0 && blockIdx.z == 0) make_schedule(p, ctas);
     return;
   }
-  const int b = blockIdx.z, h = blockIdx.y, j = threadIdx.x % kLanes, t = ((int)blockIdx.x - 1) * kTokens + threadIdx.x / kLanes;
+  const int lane = threadIdx.x % kLanes, block0 = ((int)blockIdx.x - 1) * kTokens, t = block0 + threadIdx.x / kLanes;
+  const int b = blockIdx.z, h = blockIdx.y;
   const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, p.status);
   const int used = blocks_of(ex, p.group) * kRows;           // rows, those beyond the last token zeros
-  const bool real = t < ex.fresh;
+  const bool real = t < ex.fresh, turn = real && lane < p.rope.dim >> 4;
+  const Chunks c = chunks_of<INTERLEAVED>(lane, p.rope.dim);
   // rows without a query answer nothing (every other row has a tile: it sees a key, or its block masks all of the tile)
   if (!real && t < p.m_tokens) {
     for (int g = 0; g < p.group; ++g) {
       const int head = h * p.group + g;
-      *reinterpret_cast<uint4*>(p.out + (int64_t)b * p.os.b + (int64_t)head * p.os.h + (int64_t)t * p.os.t + 8 * j) = make_uint4(0, 0, 0, 0);
-      if (p.lse && j == 0) p.lse[((int64_t)b * p.q_heads + head) * p.m_tokens + t] = -INFINITY;
+      uint4* out = reinterpret_cast<uint4*>(p.out + (int64_t)b * p.os.b + (int64_t)head * p.os.h + (int64_t)t * p.os.t + 16 * lane);
+      out[0] = out[1] = make_uint4(0, 0, 0, 0);
+      if (p.lse && lane == 0) p.lse[((int64_t)b * p.q_heads + head) * p.m_tokens + t] = -INFINITY;
     }
   }
-  if ((long long)((int)blockIdx.x - 1) * kTokens * p.group >= used) return;
+  if ((long long)block0 * p.group >= used) return;
   bool far = false;
-  Turn turn = {};
-  if (p.rope.dim && real) turn = load_turn(p.rope, rope_row(p.rope, b, t, ex.before, &far), j);
+  float cs[8], sn[8];
+  if (turn) {
+    const int64_t at = (int64_t)rope_row(p.rope, b, t, ex.before, &far) * (p.rope.dim >> 1) + 8 * lane;
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      *reinterpret_cast<float4*>(cs + i) = *reinterpret_cast<const float4*>(p.rope.cos + at + i);
+      *reinterpret_cast<float4*>(sn + i) = *reinterpret_cast<const float4*>(p.rope.sin + at + i);
+    }
+  }
   if (far) report(p.status, kBadPosition);
-  const uint16_t* q = p.q + (int64_t)b * p.qs.b + (int64_t)h * p.group * p.qs.h + (int64_t)t * p.qs.t + 8 * j;
+  const uint16_t* q = p.q + (int64_t)b * p.qs.b + (int64_t)h * p.group * p.qs.h + (int64_t)t * p.qs.t;
   const int64_t unit0 = ((int64_t)b * p.pool.kv_heads + h) * p.max_blocks;
   for (int g0 = 0; g0 < p.group; g0 += kBatch) {
-    uint4 raw[kBatch];
+    uint4 wa[kBatch], wb[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      raw[i] = make_uint4(0, 0, 0, 0);
-      if (real && g0 + i < p.group) raw[i] = *reinterpret_cast<const uint4*>(q + (int64_t)(g0 + i) * p.qs.h);
+      wa[i] = wb[i] = make_uint4(0, 0, 0, 0);
+      if (real && g0 + i < p.group) {
+        wa[i] = *reinterpret_cast<const uint4*>(q + (int64_t)(g0 + i) * p.qs.h + 8 * c.a);
+        wb[i] = *reinterpret_cast<const uint4*>(q + (int64_t)(g0 + i) * p.qs.h + 8 * c.b);
+      }
     }
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (g0 + i >= p.group) break;
-      float x[8];
-      bf16x8_to_f32(raw[i], x);
-      if (p.rope.dim) rotate8(x, turn, p.rope, j);
-      const QueryParts<2> qp = query_parts<D, 2, 1>(x);
+      float x[16];
+      unpack<INTERLEAVED>(wa[i], wb[i], x);
+      if (turn) rotate16(x, cs, sn);
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) top = max(top, __float_as_uint(x[k]) & 0x7FFFFFFFu);
+#pragma unroll
+      for (int k = kLanes / 2; k; k >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
+      // scaled to at most 448, rounded to FP16 (11 bits), cut into two E4M3 numbers (9 bits)
+      const int e = query_exponent(top);
+      const float f = pow2(-e);
+      uint32_t hi[8], lo[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int u = INTERLEAVED ? k : 2 * k, w = INTERLEAVED ? 8 + k : 2 * k + 1;
+        const uint32_t v = cvt_f16x2(x[u] * f, x[w] * f);
+        hi[k] = f16x2_to_e4m3x2(v);
+        const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&v), as_half2(e4m3x2_to_f16x2(hi[k])));
+        lo[k] = f16x2_to_e4m3x2(*reinterpret_cast<const uint32_t*>(&rest));
+      }
       const long long row = (long long)t * p.group + g0 + i;
       if (row < used) {
         const int64_t unit = unit0 + (row >> 8);
         const int r = (int)row & 127, qt = (int)(row >> 7) & 1;
-        uint8_t* to = p.queries + (unit * 2 + qt) * (2 * F::kTile) + RowLayout<D>::at(r, 8 * j);
-        *reinterpret_cast<uint2*>(to) = qp.part[0];
-        *reinterpret_cast<uint2*>(to + F::kTile) = qp.part[1];
-        if (j == 0) p.factors[unit * kRows + (row & (kRows - 1))] = qp.factor * p.scale_log2;
+        uint8_t* to = p.queries + (unit * 2 + qt) * (2 * F::kTile);
+        const uint32_t a = RowLayout<D>::at(r, 8 * c.a), d = RowLayout<D>::at(r, 8 * c.b);
+        *reinterpret_cast<uint2*>(to + a) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+        *reinterpret_cast<uint2*>(to + d) = make_uint2(hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
+        *reinterpret_cast<uint2*>(to + F::kTile + a) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+        *reinterpret_cast<uint2*>(to + F::kTile + d) = make_uint2(lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+        if (lane == 0) p.factors[unit * kRows + (row & (kRows - 1))] = (top < 0x7F800000u ? pow2(e) : __int_as_float(0x7FC00000)) * p.scale_log2;
       }
     }
   }
@@ -734,8 +773,9 @@ int launch(const AttnCall& c, const CUtensorMap& mk, const CUtensorMap& mv, cons
     KVQ_CUDA_TRY(cudaFuncSetAttribute(paged_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
     set.done(dev);
   }
-  const int64_t tokens = ((int64_t)p.max_blocks * kRows + c.group - 1) / c.group, per = kQueryThreads / (D / 8);
-  r = launch_after(true, 1, dim3((unsigned)((tokens + per - 1) / per) + 1, c.pool.kv_heads, c.seqs.batch), dim3(kQueryThreads), 0, c.stream, paged_query_kernel<D>, p, ctas);
+  const int64_t tokens = ((int64_t)p.max_blocks * kRows + c.group - 1) / c.group, per = kQueryThreads / (D / 16);
+  r = launch_after(true, 1, dim3((unsigned)((tokens + per - 1) / per) + 1, c.pool.kv_heads, c.seqs.batch), dim3(kQueryThreads), 0, c.stream,
+                   p.rope.interleaved ? paged_query_kernel<D, true> : paged_query_kernel<D, false>, p, ctas);
   if (r != KVQ_OK) return r;
   r = launch_after(true, 1, dim3(ctas), dim3(kThreads), F::kSmem, c.stream, paged_chunk_kernel<D>, mk, mv, p);
   if (r != KVQ_OK) return r;

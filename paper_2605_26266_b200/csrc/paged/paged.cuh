@@ -155,6 +155,42 @@ __device__ __forceinline__ void rotate8(float (&x)[8], const Turn& t, const Rope
   }
 }
 
+// The same with 16 channels a lane, which then needs no other: two chunks of 8 that are partners of the rotation.
+struct Chunks { int a, b; };
+template <bool INTERLEAVED>
+__device__ __forceinline__ Chunks chunks_of(int lane, int dim) {
+  const int turned = dim >> 4;
+  if (INTERLEAVED) return {2 * lane, 2 * lane + 1};
+  return lane < turned ? Chunks{lane, lane + turned} : Chunks{2 * lane, 2 * lane + 1};
+}
+// 16 channels of a token that a lane has: two chunks of 8.  x[0..7] and x[8..15] are partners of the rotation, number by number: chunks that lie dim / 2
+// channels apart, or the even and the odd channels of two neighbouring chunks.
+template <bool INTERLEAVED>
+__device__ __forceinline__ void unpack(const uint4& a, const uint4& b, float (&x)[16]) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xFFFF0000u);
+    if (INTERLEAVED) { x[i] = lo; x[8 + i] = hi; }
+    else { x[2 * i] = lo; x[2 * i + 1] = hi; }
+  }
+}
+// Every product and sum is rounded by itself: the result is that of the formulas in binary32, whoever computes them.  (Packed products and sums of
+// two numbers are made FMAs on the way to the machine, with explicit rounding too: nine codes of 14 million came out differently.)
+__device__ __forceinline__ void rotate16(float (&x)[16], const float* cs, const float* sn) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 4) {
+    const float4 c = *reinterpret_cast<const float4*>(cs + i), s = *reinterpret_cast<const float4*>(sn + i);
+    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const float u = x[i + h], w = x[8 + i + h];
+      x[i + h] = __fsub_rn(__fmul_rn(u, cc[h]), __fmul_rn(w, ss[h]));
+      x[8 + i + h] = __fadd_rn(__fmul_rn(w, cc[h]), __fmul_rn(u, ss[h]));
+    }
+  }
+}
+
 __device__ __forceinline__ void bf16x8_to_f32(const uint4& w, float (&x)[8]) {
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll

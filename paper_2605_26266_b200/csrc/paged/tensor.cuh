@@ -61,16 +61,18 @@ int make_pool_map(CUtensorMap* map, const void* codes, const Pool& pool, int hea
 // Cycles a wait may take (kvq_set_wait_budget_cycles).
 uint32_t wait_budget();
 
+// Exponent of a row of queries whose largest magnitude has these bits: the smallest that keeps it at 448 or less, from -100 up.
+__device__ __forceinline__ int query_exponent(uint32_t top) { return max((int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u), -100); }
+
 // A row of queries: 8 channels of a lane, D / 8 neighbouring lanes a row.  Rotated, scaled by a power of two to at most 448 and cut
-// into PARTS E4M3 numbers, part i of them times STEP^i (1 where one accumulator takes all parts); with two parts 9 bits of each channel (a BF16 that is not rotated is exact), with
-// three 13.  `factor` is what a product with the parts, part i divided by STEP^i, has to be multiplied by; it is NaN for a
+// into PARTS E4M3 numbers, part i of them times 16^i; three carry 13 bits of each channel.  `factor` is what a product with the parts, part i divided by 16^i, has to be multiplied by; it is NaN for a
 // row with a channel that is no finite number, whose scores then are none either.
 template <int PARTS>
 struct QueryParts {
   uint2 part[PARTS];
   float factor;
 };
-template <int D, int PARTS, int STEP = 16>
+template <int D, int PARTS>
 __device__ __forceinline__ QueryParts<PARTS> query_parts(float (&x)[8]) {
   QueryParts<PARTS> r;
   uint32_t top = 0;
@@ -78,7 +80,7 @@ __device__ __forceinline__ QueryParts<PARTS> query_parts(float (&x)[8]) {
   for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
 #pragma unroll
   for (int i = D / 16; i; i >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, i));
-  const int e = max((int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u), -100);
+  const int e = query_exponent(top);
   const float f = pow2(-e);
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] *= f;
@@ -90,8 +92,8 @@ __device__ __forceinline__ QueryParts<PARTS> query_parts(float (&x)[8]) {
       const uint32_t lo = e4m3x2(x[4 * h], x[4 * h + 1]), hi = e4m3x2(x[4 * h + 2], x[4 * h + 3]);
       w[h] = lo | hi << 16;
       const float2 a = e4m3x2_to_f32(lo), b = e4m3x2_to_f32(hi);
-      x[4 * h] = (x[4 * h] - a.x) * STEP; x[4 * h + 1] = (x[4 * h + 1] - a.y) * STEP;
-      x[4 * h + 2] = (x[4 * h + 2] - b.x) * STEP; x[4 * h + 3] = (x[4 * h + 3] - b.y) * STEP;
+      x[4 * h] = (x[4 * h] - a.x) * 16.f; x[4 * h + 1] = (x[4 * h + 1] - a.y) * 16.f;
+      x[4 * h + 2] = (x[4 * h + 2] - b.x) * 16.f; x[4 * h + 3] = (x[4 * h + 3] - b.y) * 16.f;
     }
     r.part[p] = make_uint2(w[0], w[1]);
   }
