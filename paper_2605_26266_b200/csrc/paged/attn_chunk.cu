@@ -39,14 +39,15 @@ struct ChunkParams {
   uint8_t* queries;                // [batch][key head][row block][query tile]: two parts of 128 rows as they lie in shared memory
   float* factors;                  // [batch][key head][row block][256]
   int max_blocks;                  // row blocks of m_tokens
+  int out_32;                      // rows of the output start on 32-byte boundaries
   int4* places;                    // [CTAs][2]: where a CTA's tile steps begin
-  long long* upto;                 // [batch]: tile steps of the sequences up to and with this one
+  long long* upto;                 // [batch]: steps of the sequences up to and with this one
   uint32_t wait_budget;
 };
 
 constexpr int kThreads = 512;      // producer, two issuers, queries; two softmax groups; expanding warps
 constexpr int kRows = 256;
-constexpr int kRegsIssue = 72, kRegsSoftmax = 168, kRegsExpand = 104;      // 128 (72 + 2 * 168 + 104) = 512 * 128
+constexpr int kRegsIssue = 48, kRegsSoftmax = 192, kRegsExpand = 80;      // 128 (48 + 2 * 192 + 80) = 512 * 128
 constexpr float kBase = 4.f, kSlack = 8.f, kNoMax = -1e30f, kLeast = 1.17549435e-38f;
 enum { kNone = 0, kStart = 1, kMiddle = 2, kEnd = 3 };
 
@@ -60,8 +61,8 @@ struct Chunk {
   static constexpr int kOffV = kOffRaw + kRawStages * kTile;        // FP16
   static constexpr int kOffBar = kOffV + kVStages * 2 * kTile;
   enum { kKFull = 0, kKEmpty = kKFull + kKStages, kRawFull = kKEmpty + kKStages, kRawEmpty = kRawFull + kRawStages, kVFull = kRawEmpty + kRawStages,
-         kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPFull = kSFull + 4, kODone = kPFull + 4,
-         kOFree = kODone + 4, kDrain = kOFree + 2, kBars = kDrain + 2 };        // of scores, weights and products: + 2 half + query tile
+         kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPFull = kSFull + 2, kODone = kPFull + 4,      // of weights: + 2 half + query tile
+         kOFree = kODone + 2, kTurn = kOFree + 2, kDrain = kTurn + 2, kBars = kDrain + 2 };
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kOffScale = (kOffMisc + 8 + 127) / 128 * 128;      // [8 tiles][3][8] floats: key factors, value exponents, their inverses
   static constexpr int kSmem = kOffScale + 8 * 96 + 1024;
@@ -69,8 +70,13 @@ struct Chunk {
   static constexpr int kSlotBytes = kSlotStats + 2 * kRows * 4;
 };
 
-// A row block of a sequence and a CTA's place in the line of tile steps.
-struct Place { int b, h, rb, t; long long left; };
+// The line of tile steps: a unit counts kUnitSteps for its start and end, which take about as long (outputs, first loads and scores: 8 000 to 10 000 cycles;
+// without them CTAs with the short first blocks of causal prompts took 1.3 times as long as the others), then one for each tile.
+constexpr int kUnitSteps = 2;
+__device__ __forceinline__ int tile_at(long long steps, int tiles) { return (int)min((long long)tiles, max(steps - kUnitSteps, 0ll)); }
+
+// A CTA's place in the line: a unit, the steps of it that are behind, and the CTA's steps.
+struct Place { int b, h, rb, behind; long long left; };
 struct Segment { int b, h, rb, tb, te, n, first; Extent ex; };
 
 // Row blocks of a sequence, and the key tiles of one.
@@ -101,12 +107,13 @@ struct Walker {
         if (++at.h == p.pool.kv_heads || blocks == 0) { at.h = 0; ++at.b; known = false; }
       }
     }
-    s.b = at.b; s.h = at.h; s.rb = at.rb; s.tb = at.t; s.n = tl.count; s.first = tl.first; s.ex = ex;
-    s.te = (int)min((long long)tl.count, at.t + at.left);
-    at.left -= s.te - s.tb;
-    at.t = 0;
+    s.b = at.b; s.h = at.h; s.rb = at.rb; s.n = tl.count; s.first = tl.first; s.ex = ex;
+    s.tb = tile_at(at.behind, tl.count);
+    s.te = tile_at(at.behind + at.left, tl.count);
+    at.left -= tl.count + kUnitSteps - at.behind;
+    at.behind = 0;
     ++at.rb;
-    return true;
+    return s.te > s.tb;                                         // a range may end in a unit's start
   }
 };
 
@@ -122,7 +129,7 @@ struct Blocks {
   }
 };
 
-// One block: the line of tile steps (sequence, key head, row block, tile), cut evenly.
+// One block: the line of steps (sequence, key head, row block, tile), cut evenly.
 __device__ void make_schedule(const ChunkParams& p, int ctas) {
   __shared__ long long s_sum[kRows];
   const int tid = threadIdx.x;
@@ -135,9 +142,9 @@ __device__ void make_schedule(const ChunkParams& p, int ctas) {
       const int blocks = blocks_of(ex, p.group);
       if (p.causal) {
         Blocks it(ex, p.group);
-        for (int rb = 0; rb < blocks; ++rb) mine += it.next(ex, p);
+        for (int rb = 0; rb < blocks; ++rb) mine += it.next(ex, p) + kUnitSteps;
       } else {
-        mine = (long long)blocks * tiles_of(ex, 0, 1, 0, 0).count;
+        mine = (long long)blocks * (tiles_of(ex, 0, 1, 0, 0).count + kUnitSteps);
       }
     }
     s_sum[tid] = mine * p.pool.kv_heads;
@@ -170,13 +177,13 @@ __device__ void make_schedule(const ChunkParams& p, int ctas) {
       const Extent ex = extent_of(p.seqs, p.pool.page, r.b, p.m_tokens, nullptr);
       Blocks it(ex, p.group);
       for (;; ++r.rb) {
-        const int count = p.causal ? it.next(ex, p) : tiles_of(ex, 0, 1, 0, 0).count;
+        const int count = (p.causal ? it.next(ex, p) : tiles_of(ex, 0, 1, 0, 0).count) + kUnitSteps;
         if (in < count) break;
         in -= count;
       }
-      r.t = (int)in;
+      r.behind = (int)in;
     }
-    p.places[2 * c] = make_int4(r.b, r.h, r.rb, r.t);
+    p.places[2 * c] = make_int4(r.b, r.h, r.rb, r.behind);
     p.places[2 * c + 1] = make_int4((int)r.left, (int)(r.left >> 32), 0, 0);
   }
 }
@@ -186,10 +193,15 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// tcgen05.wait::ld with the registers of a load that was issued long before: nothing that uses them may come ahead of it.
-__device__ __forceinline__ void tmem_wait_ld_of(uint32_t* r) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]),"+r"(r[1]),"+r"(r[2]),"+r"(r[3]),"+r"(r[4]),"+r"(r[5]),"+r"(r[6]),"+r"(r[7]),"+r"(r[8]),"+r"(r[9]),"+r"(r[10]),"+r"(r[11]),"+r"(r[12]),"+r"(r[13]),"+r"(r[14]),"+r"(r[15]),"+r"(r[16]),"+r"(r[17]),"+r"(r[18]),"+r"(r[19]),"+r"(r[20]),"+r"(r[21]),"+r"(r[22]),"+r"(r[23]),"+r"(r[24]),"+r"(r[25]),"+r"(r[26]),"+r"(r[27]),"+r"(r[28]),"+r"(r[29]),"+r"(r[30]),"+r"(r[31]) :: "memory");
+// tcgen05.st of 32 columns that does not order the memory accesses around it
+__device__ __forceinline__ void st32_plain(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]));
 }
 __device__ __forceinline__ bool all_lanes(bool x) { return __all_sync(0xFFFFFFFFu, x); }
 
@@ -320,10 +332,9 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     for (int s = 0; s < 2; ++s) {
       mbar_init(cx.bar(F::kRawFull + s), 1); mbar_init(cx.bar(F::kRawEmpty + s), 128);
       mbar_init(cx.bar(F::kVFull + s), 128); mbar_init(cx.bar(F::kVEmpty + s), 2);
-      mbar_init(cx.bar(F::kQFull + s), 1); mbar_init(cx.bar(F::kOFree + s), 128); mbar_init(cx.bar(F::kDrain + s), 1);
-    }
-    for (int s = 0; s < 4; ++s) {
-      mbar_init(cx.bar(F::kSFull + s), 1); mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kODone + s), 1);
+      mbar_init(cx.bar(F::kQFull + s), 1); mbar_init(cx.bar(F::kOFree + s), 128);
+      mbar_init(cx.bar(F::kSFull + s), 1); mbar_init(cx.bar(F::kODone + s), 1); mbar_init(cx.bar(F::kTurn + s), 1); mbar_init(cx.bar(F::kDrain + s), 1);
+      mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kPFull + 2 + s), 128);
     }
     mbar_init(cx.bar(F::kQEmpty), 2);
     fence_barrier_init();
@@ -339,8 +350,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + F::kOffMisc);
   const int4 at = load_coherent(p.places + 2 * blockIdx.x), left = load_coherent(p.places + 2 * blockIdx.x + 1);
   const Place place{at.x, at.y, at.z, at.w, (long long)(uint32_t)left.x | (long long)left.y << 32};
-  // TMEM columns: S0 [0,128) S1 [128,256) O0 [256, 256 + D) O1 [384, 384 + D); a key tile is two halves of 64 keys with 64 columns each,
-  // and weights (FP16 pairs) lie over the first 32 columns of their half's scores.
+  // TMEM columns: S0 [0,128) S1 [128,256) O0 [256, 256 + D) O1 [384, 384 + D); weights (FP16 pairs) over the first 64 columns of their scores.
 
   if (warp < 4) {
     setmaxnreg_dec<kRegsIssue>();
@@ -414,7 +424,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       // ================= issuers: warp 1 + qt for query tile qt =================
       const bool leader = elect_one();
       const int qt = warp - 1;
-      const uint32_t idesc_s = make_idesc_e4m3(128, 64, 0, 0);
+      const uint32_t idesc_s = make_idesc_e4m3(128, 128, 0, 0);
       const uint32_t idesc_o = make_idesc_bf16(128, D, 0, 1) & ~((7u << 7) | (7u << 10));      // FP16
       const uint64_t dq = make_smem_desc(sbase + F::kOffQ + qt * 2 * F::kTile, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
       const uint64_t dk = make_smem_desc(sbase + F::kOffK, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
@@ -422,59 +432,77 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const uint32_t s_tmem = tmem + qt * 128, o_tmem = tmem + 256 + qt * 128;
       Walker w(place);
       Segment sg;
-      int it = 0, n = 0, nseg = 0, nact = 0;                   // tiles, tiles and segments of this query tile
+      int it = 0, n = 0, nseg = 0, nact = 0, turns = 0;        // tiles, tiles and segments of this query tile, its turns
       bool ok = true;
-      // Per half of a tile: O += P V over its 64 keys, then at once the same half's scores of the next tile, into the columns that P has left: the tensor
-      // pipe executes one thread's products in order.  So a softmax group has the other half to work on while its next scores are computed.
+      auto scores = [&](int i) {                               // of tile i
+        if (!leader) return;
+        const int s = i % F::kKStages;
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k)
+            mma_e4m3_ss(s_tmem, dq + (uint64_t)((part * F::kTile + 32 * k) >> 4), dk + (uint64_t)((s * F::kTile + 32 * k) >> 4), idesc_s, part + k > 0);
+        tc_commit(cx.bar(F::kSFull + qt));
+      };
+      auto products = [&](int s, int hf, bool add) {           // of 64 keys of stage s
+        if (!leader) return;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)                            // 16 keys a step
+          mma_ts(o_tmem, s_tmem + 32 * hf + 8 * k, dv + (uint64_t)((s * 2 * F::kTile + (4 * hf + k) * 16 * 128) >> 4), idesc_o, add || k > 0);
+      };
+      // The two query tiles take turns at the tensor pipe: O += P V of one and at once its next scores, then the same of the other.  That keeps the softmax groups
+      // half a step apart: one has its exponentials while the other waits for products.  Each has its own warp, whose waits and commits then do not hold up
+      // the other's products.
+      auto my_turn = [&](bool both) -> bool {
+        if (!both) return true;
+        const bool r = all_lanes(cx.wait(F::kTurn + qt, (turns & 1) ^ 1 ^ qt, 716));
+        ++turns;
+        return r;
+      };
+      auto pass_on = [&](bool both) {
+        if (both && leader) mbar_arrive(cx.bar(F::kTurn + (qt ^ 1)));
+        __syncwarp();
+      };
       while (ok && w.next(sg, p)) {
-        const bool act = sg.ex.fresh * p.group - sg.rb * kRows > qt * 128;
-        if (!(ok = all_lanes(cx.wait(F::kQFull + qt, nseg & 1, 712)))) break;
-        for (int t = sg.tb - 1; t < sg.te && ok; ++t) {
-          const bool product = t >= sg.tb, next = t + 1 < sg.te;
-          const int i1 = product ? it + 1 : it, s1 = i1 % F::kKStages, vs = it & 1;
-#pragma unroll 1
-          for (int hf = 0; hf < 2; ++hf) {
-            if (product) {
-              if (hf == 0 && !(ok = all_lanes(cx.wait(F::kVFull + vs, it >> 1 & 1, 713)))) break;
-              if (act) {
-                if (hf == 0 && t == sg.tb && !(ok = all_lanes(cx.wait(F::kOFree + qt, (nact & 1) ^ 1, 714)))) break;
-                if (!(ok = all_lanes(cx.wait(F::kPFull + 2 * hf + qt, n & 1, 715)))) break;
-                tc_fence_after();
-                if (leader) {
-#pragma unroll
-                  for (int k = 0; k < 4; ++k)                  // 16 keys a step
-                    mma_ts(o_tmem, s_tmem + 64 * hf + 8 * k, dv + (uint64_t)((vs * 2 * F::kTile + (4 * hf + k) * 16 * 128) >> 4), idesc_o, t > sg.tb || hf > 0 || k > 0);
-                  tc_commit(cx.bar(F::kODone + 2 * hf + qt));
-                }
-              }
-              if (hf == 1 && leader) tc_commit(cx.bar(F::kVEmpty + vs));
-              __syncwarp();
-            }
-            if (next) {
-              if (hf == 0 && !(ok = all_lanes(cx.wait(F::kKFull + s1, i1 / F::kKStages & 1, 711)))) break;
-              tc_fence_after();
-              if (leader) {
-                if (act) {
-#pragma unroll
-                  for (int part = 0; part < 2; ++part)
-#pragma unroll
-                    for (int k = 0; k < D / 32; ++k)
-                      mma_e4m3_ss(s_tmem + 64 * hf, dq + (uint64_t)((part * F::kTile + 32 * k) >> 4), dk + (uint64_t)((s1 * F::kTile + hf * 64 * D + 32 * k) >> 4), idesc_s, part + k > 0);
-                  tc_commit(cx.bar(F::kSFull + 2 * hf + qt));
-                }
-                if (hf == 1) {
-                  tc_commit(cx.bar(F::kKEmpty + s1));
-                  if (t + 2 == sg.te) tc_commit(cx.bar(F::kQEmpty));
-                }
-              }
-              __syncwarp();
-            }
-          }
-          if (product) {
-            ++it;
-            if (act) ++n;
-          }
+        const int rows = sg.ex.fresh * p.group - sg.rb * kRows;
+        const bool act = rows > qt * 128, both = rows > 128;
+        if (!(ok = all_lanes(cx.wait(F::kQFull + qt, nseg & 1, 712)) && all_lanes(cx.wait(F::kKFull + it % F::kKStages, it / F::kKStages & 1, 711)))) break;
+        if (!(ok = my_turn(both))) break;
+        tc_fence_after();
+        if (act) scores(it);
+        pass_on(both);
+        if (leader) {
+          tc_commit(cx.bar(F::kKEmpty + it % F::kKStages));
+          if (sg.te - sg.tb == 1) tc_commit(cx.bar(F::kQEmpty));
         }
+        __syncwarp();
+        for (int t = sg.tb; t < sg.te; ++t, ++it) {
+          const int vs = it & 1, s1 = (it + 1) % F::kKStages;
+          const bool next = t + 1 < sg.te;
+          if (!(ok = all_lanes(cx.wait(F::kVFull + vs, it >> 1 & 1, 713)))) break;
+          if (next && !(ok = all_lanes(cx.wait(F::kKFull + s1, (it + 1) / F::kKStages & 1, 711)))) break;
+          if (act) {
+            if (t == sg.tb && !(ok = all_lanes(cx.wait(F::kOFree + qt, (nact & 1) ^ 1, 714)))) break;
+            if (!(ok = all_lanes(cx.wait(F::kPFull + qt, n & 1, 715)))) break;
+            if (!(ok = my_turn(both))) break;
+            tc_fence_after();
+            products(vs, 0, t > sg.tb);
+            if (!(ok = all_lanes(cx.wait(F::kPFull + 2 + qt, n & 1, 717)))) break;
+            tc_fence_after();
+            products(vs, 1, true);
+            if (leader && !next) tc_commit(cx.bar(F::kODone + qt));
+            if (next) scores(it + 1);
+            pass_on(both);
+            ++n;
+          }
+          if (leader) {
+            tc_commit(cx.bar(F::kVEmpty + vs));
+            if (next) tc_commit(cx.bar(F::kKEmpty + s1));
+            if (t + 2 == sg.te) tc_commit(cx.bar(F::kQEmpty));
+          }
+          __syncwarp();
+        }
+        if (!ok) break;
         ++nseg;
         if (act) ++nact;
       }
@@ -485,11 +513,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       if (ok) {
         for (int k = max(it - F::kKStages, 0); k < it; ++k) cx.drain(F::kKEmpty + k % F::kKStages, k / F::kKStages & 1);
         for (int k = max(it - 2, 0); k < it; ++k) cx.drain(F::kVEmpty + (k & 1), k >> 1 & 1);
-        if (n > 0)
-          for (int hf = 0; hf < 2; ++hf) { cx.drain(F::kSFull + 2 * hf + qt, (n - 1) & 1); cx.drain(F::kODone + 2 * hf + qt, (n - 1) & 1); }
+        if (n > 0) { cx.drain(F::kSFull + qt, (n - 1) & 1); cx.drain(F::kODone + qt, (nact - 1) & 1); }
         if (nseg > 0) cx.drain(F::kQEmpty, (nseg - 1) & 1);
       }
-    } else {
+    } else if (warp == 3) {
       // ================= queries =================
       Walker w(place);
       Segment sg;
@@ -521,7 +548,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     if (tid == 128) header[0] = header[1] = make_int4(kNone, 0, 0, 0);
     Walker w(place);
     Segment sg;
-    int it = 0, n = 0, nseg = 0;
+    int it = 0, n = 0, nseg = 0, nact = 0;
     bool ok = true;
     while (ok && w.next(sg, p)) {
       const int rows = sg.ex.fresh * p.group - sg.rb * kRows;        // of this block and after it
@@ -533,44 +560,42 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const int hi = real ? (p.causal ? pos + 1 : total) : 0x7FFFFFFF, lo = real && p.window ? pos + 1 - p.window : 0;      // keys [lo, hi) are seen
       float m = kNoMax, l = 0.f;
       const float rowf = load_coherent(p.factors + (((int64_t)sg.b * p.pool.kv_heads + sg.h) * p.max_blocks + sg.rb) * kRows + r256);
-      uint32_t s[64];
-      float f[4], v[4], inv[4];
-      auto fetch = [&](uint32_t (&s)[64], int hf, int i) -> bool {                  // scores of half hf of this query tile's tile i
-        if (!all_lanes(cx.wait(F::kSFull + 2 * hf + qt, i & 1, 721))) return false;
+#pragma unroll 1
+      for (int t = sg.tb; t < sg.te; ++t, ++it, ++n) {
+        ok = all_lanes(cx.wait(F::kSFull + qt, n & 1, 721));
+        if (!ok) break;
         tc_fence_after();
-        tmem_ld32(s_addr + 64 * hf, s);
-        tmem_ld32(s_addr + 64 * hf + 32, s + 32);
-        return true;
-      };
-      // masks, factors and the running maximum of half hf of tile t (the it-th of the CTA, the n-th of the query tile)
-      auto prepare = [&](uint32_t (&s)[64], int hf, int t, int it, int n) -> bool {
-        const float4* sc = reinterpret_cast<const float4*>(smem + F::kOffScale) + (it & 7) * 6 + hf;
-        const float4 f4 = sc[0], v4 = sc[2], i4 = sc[4];
-        // not 0: a hidden score is -inf, and -inf * 0 would be none (a row of no finite numbers is dealt with at the end)
-        f[0] = fmaxf(f4.x * rowf, kLeast); f[1] = fmaxf(f4.y * rowf, kLeast); f[2] = fmaxf(f4.z * rowf, kLeast); f[3] = fmaxf(f4.w * rowf, kLeast);
-        v[0] = v4.x; v[1] = v4.y; v[2] = v4.z; v[3] = v4.w;
-        inv[0] = i4.x; inv[1] = i4.y; inv[2] = i4.z; inv[3] = i4.w;
-        tmem_wait_ld_of(s);
-        tmem_wait_ld_of(s + 32);
-        const int first = (sg.first + t) * kTileKeys + 64 * hf;
-        if (__any_sync(0xFFFFFFFFu, first + 64 > hi || first < lo) || first + 64 > total) {
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) tmem_ld32(s_addr + c, s + c);
+        const float4* sc = reinterpret_cast<const float4*>(smem + F::kOffScale) + (it & 7) * 6;      // of 16 keys each: factors, exponents, inverses
+        const int first = (sg.first + t) * kTileKeys;
+        const bool edge = __any_sync(0xFFFFFFFFu, first + kTileKeys > hi || first < lo) || first + kTileKeys > total;
+        float f[8], v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 f4 = sc[h], v4 = sc[2 + h];
+          // not 0: a hidden score is -inf, and -inf * 0 would be none (a row of no finite numbers is dealt with at the end)
+          f[4 * h] = fmaxf(f4.x * rowf, kLeast); f[4 * h + 1] = fmaxf(f4.y * rowf, kLeast); f[4 * h + 2] = fmaxf(f4.z * rowf, kLeast); f[4 * h + 3] = fmaxf(f4.w * rowf, kLeast);
+          v[4 * h] = v4.x; v[4 * h + 1] = v4.y; v[4 * h + 2] = v4.z; v[4 * h + 3] = v4.w;
+        }
+        tmem_wait_ld();
+        if (edge) {
           const int nv = min(hi, total) - first, nl = lo - first;
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
+          for (int i = 0; i < 128; ++i)
             if (i >= nv || i < nl) s[i] = 0xFF800000u;
         }
         float m_new = m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
           auto at = [&](int j) { return __uint_as_float(s[16 * i + j]); };
           const float a = max3(max3(at(0), at(1), at(2)), at(3), at(4)), b = max3(max3(at(5), at(6), at(7)), at(8), at(9));
           const float c = max3(max3(at(10), at(11), at(12)), at(13), at(14));
           m_new = fmaxf(m_new, fmaf(max3(a, b, fmaxf(c, at(15))), f[i], v[i]));
         }
         if (__any_sync(0xFFFFFFFFu, m_new - m > kSlack)) {
-          if (t > sg.tb || hf > 0) {
-            if (!all_lanes(cx.wait(F::kODone + 2 * (hf ^ 1) + qt, (n - (hf ^ 1)) & 1, 722))) return false;      // the last product on O
-            tc_fence_after();
+          if (t > sg.tb) {                             // the last product on O is done: the commit of these scores came after it
             const float drop = ex2(m - m_new);
 #pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
@@ -585,39 +610,39 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           }
           m = m_new;
         }
-        return true;
-      };
-      auto weights = [&](uint32_t (&s)[64], int hf) {
+        // weights; nothing in between that orders memory, so that one piece's exponentials run into the next one's
+        const float4 ia = sc[4], ib = sc[5];
+        const float inv[8] = {ia.x, ia.y, ia.z, ia.w, ib.x, ib.y, ib.z, ib.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 f2 = make_float2(f[i], f[i]);
-          const float b = v[i] - m + kBase;
-          const float2 b2 = make_float2(b, b);
+        for (int i = 0; i < 8; ++i) v[i] = v[i] - m + kBase;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 ff = make_float2(f[i], f[i]), bb = make_float2(v[i], v[i]);
           float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
           for (int j = 0; j < 16; j += 2) {
-            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[16 * i + j]), __uint_as_float(s[16 * i + j + 1])), f2, b2);
+            const int k = 16 * i + j;
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), ff, bb);
             const float2 w2 = make_float2(ex2(x.x), ex2(x.y));
             sum = __fadd2_rn(sum, w2);
-            s[8 * i + j / 2] = cvt_f16x2(w2.x, w2.y);
+            s[k / 2] = cvt_f16x2(w2.x, w2.y);
           }
           l = fmaf(sum.x + sum.y, inv[i], l);
+          if (i == 3) st32_plain(s_addr, s);
+          if (i == 5) {
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(cx.bar(F::kPFull + qt));
+          }
         }
-        tmem_st32(s_addr + 64 * hf, s);
+        tmem_st32(s_addr + 32, s + 32);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(cx.bar(F::kPFull + 2 * hf + qt));
-      };
-#pragma unroll 1
-      for (int i = 0; i < 2 * (sg.te - sg.tb); ++i) {
-        const int hf = i & 1, t = sg.tb + (i >> 1);
-        if (!(ok = fetch(s, hf, n) && prepare(s, hf, t, it, n))) break;
-        weights(s, hf);
-        it += hf; n += hf;
+        mbar_arrive(cx.bar(F::kPFull + 2 + qt));
       }
       if (!ok) break;
       // ---- the rows' results ----
-      ok = all_lanes(cx.wait(F::kODone + 2 + qt, (n - 1) & 1, 723));      // the last product: a second half
+      ok = all_lanes(cx.wait(F::kODone + qt, nact & 1, 723));            // the segment's last product
       if (!ok) break;
       tc_fence_after();
       if (!(rowf == rowf)) l = rowf;                             // a query that is no finite number
@@ -640,6 +665,15 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 #pragma unroll
           for (int i = 0; i < 32; i += 4)
             *reinterpret_cast<uint4*>(to + ((size_t)((c + i) / 4) * kRows + r256) * 16) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+        } else if (real && p.out_32) {                           // whole sectors: a lane has a row, the 32 of a store meet 32 lines
+#pragma unroll
+          for (int i = 0; i < 32; i += 16) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = cvt_bf16x2(__uint_as_float(r[i + 2 * j]) * norm, __uint_as_float(r[i + 2 * j + 1]) * norm);
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         ::"l"(out + c + i), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+          }
         } else if (real) {
 #pragma unroll
           for (int i = 0; i < 32; i += 8) {
@@ -659,7 +693,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       } else if (real && p.lse) {
         p.lse[((int64_t)sg.b * p.q_heads + head) * p.m_tokens + tok] = (log2f(l) + m - kBase) * 0.6931471805599453f;
       }
-      ++nseg;
+      ++nseg; ++nact;
     }
     tc_fence_before();
   } else {
@@ -805,6 +839,7 @@ int launch_attn_chunk(const AttnCall& c) {
   p.scale_log2 = c.softmax_scale * 1.4426950408889634f;
   p.causal = c.causal; p.window = (int)c.window; p.lse = c.lse; p.status = c.status;
   p.max_blocks = (int)max_blocks(c.group, c.m_tokens);
+  p.out_32 = reinterpret_cast<uintptr_t>(c.out) % 32 == 0 && c.os.b % 16 == 0 && c.os.h % 16 == 0 && c.os.t % 16 == 0;
   const Areas a = areas_of(sms, c.head_dim, c.seqs.batch, c.pool.kv_heads, p.max_blocks);
   uint8_t* ws = static_cast<uint8_t*>(c.workspace);
   p.headers = reinterpret_cast<int4*>(ws);
