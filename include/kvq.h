@@ -313,8 +313,8 @@ int kvq_unpack_codes(const kvq_cache_desc* desc, int which, int64_t begin, int64
  * 402 (query tile, for the bias rows), 403 (query buffer free, in a part of a unit without cached tiles), 404 (value stage
  * free), 406 (packed tile in the ring).
  *
- * kvq_status_word_result maps a status word read back by the caller (host value) to KVQ_OK (0) or
- * KVQ_ERR_TIMEOUT (anything else).
+ * kvq_status_word_result maps a status word read back by the caller (host value) to KVQ_OK (0),
+ * KVQ_ERR_INVALID_ARG (faults of the lists of a paged call) or KVQ_ERR_TIMEOUT (anything else).
  * kvq_set_wait_budget_cycles sets the budget, in SM clock cycles, for kernels launched afterwards by this
  * process (0 restores the default; values above 0xFFFF0000 are KVQ_ERR_INVALID_ARG).  It exists so that the
  * time-out path can be exercised on purpose: with a budget of a few cycles the first wait that is not complete
@@ -374,7 +374,12 @@ typedef struct kvq_rope {
 /* What these calls leave in their status word (optional device int32, zero on entry; the first one is kept).  The call has done what it
  * could, and touched nothing out of bounds: 501 a page number that the pool does not have (its tokens are not written, not seen), 502 a
  * position that the tables do not have (the nearest row stands for it), 503 lengths that are negative or longer than the table row
- * (what it cannot hold is left out). */
+ * (what it cannot hold is left out).  kvq_status_word_result() gives KVQ_ERR_INVALID_ARG for these three.
+ * kvq_paged_attn also leaves the code of a bounded wait that expired, as described there; the output is then undefined.
+ * Few rows: 601 (stage free); 611 (tile), 612 (scores read), 613 (queries), 614 (weights); 621 (tile), 622 (scores), 623, 624 and 625 (product retired
+ * before a rescale, before new weights, before the sums); 631 (queries free).  Chunks: 701, 702 (stage of keys, of values free), 703 (queries free);
+ * 711 (keys), 712 (queries), 713 (values), 714 (output read out), 715 and 717 (weights of the first and second half), 716 (turn of the
+ * query tile); 721 (scores), 723 (last product); 732 (values), 733 (expanded values' stage free). */
 #define KVQ_PAGED_BAD_PAGE      501
 #define KVQ_PAGED_BAD_POSITION  502
 #define KVQ_PAGED_BAD_LENGTH    503

@@ -170,7 +170,10 @@ const char* kvq_status_string(int status) {
   }
 }
 
-int kvq_status_word_result(int32_t word) { return word == 0 ? KVQ_OK : KVQ_ERR_TIMEOUT; }
+int kvq_status_word_result(int32_t word) {
+  if (word == KVQ_PAGED_BAD_PAGE || word == KVQ_PAGED_BAD_POSITION || word == KVQ_PAGED_BAD_LENGTH) return KVQ_ERR_INVALID_ARG;
+  return word == 0 ? KVQ_OK : KVQ_ERR_TIMEOUT;
+}
 
 int kvq_set_wait_budget_cycles(uint64_t cycles) {
   if (cycles > 0xFFFF0000ull) return KVQ_ERR_INVALID_ARG;     // waits compare 32-bit clock differences

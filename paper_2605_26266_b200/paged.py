@@ -1,0 +1,129 @@
+"""Requests of different lengths over the paged 8-bit cache: who has which page, and a small rollout that uses the two calls.
+
+`Sequences` is host-side bookkeeping alone: pages are handed out as requests grow and come back when they end; the page table and the
+lengths it keeps on the device are what kvq_paged_append and kvq_paged_attn take, and every layer of a step shares them.
+
+    seqs = Sequences(slots=8, pages=4096, page=64, max_tokens=32768)
+    seqs.extend({0: 700, 1: 33})                    # room for the next step's tokens of slots 0 and 1
+    for cache, layer in ...:                        # one binding.PagedCache a layer
+        B.kvq_paged_append(cache, k, v, seqs.page_table, seqs.lengths, n_new=seqs.n_new, cos=cos, sin=sin)
+        out = B.kvq_paged_attn(cache, q, seqs.page_table, seqs.lengths, scale, n_new=seqs.n_new, cos=cos, sin=sin)
+    seqs.commit()                                   # the step's tokens are in the cache now
+    seqs.release(1)                                 # request 1 has ended: its pages can be given to others
+"""
+from __future__ import annotations
+
+import torch
+
+
+class Sequences:
+    def __init__(self, slots: int, pages: int, page: int, max_tokens: int, device="cuda"):
+        width = -(-max_tokens // page)
+        self.page, self.max_tokens = page, max_tokens
+        self._free = list(range(pages - 1, -1, -1))
+        self._held = [[] for _ in range(slots)]
+        self._len, self._new = [0] * slots, [0] * slots
+        self.page_table = torch.full((slots, width), -1, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(slots, dtype=torch.int32, device=device)
+        self.n_new = torch.zeros(slots, dtype=torch.int32, device=device)
+
+    @property
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    def extend(self, new: dict[int, int]) -> int:
+        """Room for `new[slot]` tokens of the named slots in the next step (none of the others); returns the largest count, the
+        tokens of the step's tensors.  Raises, and changes nothing, where the pool or a table row has no room for all of them."""
+        need = {s: -(-(self._len[s] + n) // self.page) - len(self._held[s]) for s, n in new.items()}
+        if any(n < 0 for n in new.values()):
+            raise ValueError("a count of new tokens is negative")
+        if any(self._len[s] + n > self.max_tokens for s, n in new.items()):
+            raise ValueError("a sequence would grow beyond max_tokens")
+        if sum(max(n, 0) for n in need.values()) > len(self._free):
+            raise MemoryError("the pool has no pages left")
+        for s, count in need.items():
+            if count > 0:
+                pages = [self._free.pop() for _ in range(count)]
+                at = len(self._held[s])
+                self._held[s] += pages
+                self.page_table[s, at:at + count] = torch.tensor(pages, dtype=torch.int32)
+        self._new = [new.get(s, 0) for s in range(len(self._len))]
+        self.n_new.copy_(torch.tensor(self._new, dtype=torch.int32))
+        return max(self._new)
+
+    def commit(self) -> None:
+        """The tokens of the last extend() have been appended (by all layers): they count as earlier ones from now on."""
+        self.lengths += self.n_new
+        self._len = [a + b for a, b in zip(self._len, self._new)]
+        self._new = [0] * len(self._len)
+        self.n_new.zero_()
+
+    def release(self, slot: int) -> None:
+        """The request in `slot` has ended: its pages are free, the slot holds an empty sequence."""
+        self._free += reversed(self._held[slot])
+        self._held[slot], self._len[slot], self._new[slot] = [], 0, 0
+        self.page_table[slot] = -1
+        self.lengths[slot] = 0
+        self.n_new[slot] = 0
+
+
+def rope_tables(rows: int, dim: int, base: float = 10000.0, device="cuda"):
+    """cos and sin, float32 [rows, dim / 2], of the usual geometric frequencies."""
+    inv = base ** (-torch.arange(0, dim, 2, dtype=torch.float64) / dim)
+    angle = torch.arange(rows, dtype=torch.float64)[:, None] * inv
+    return angle.cos().float().to(device), angle.sin().float().to(device)
+
+
+def rollout(prompts=(700, 33, 1, 260), steps=8, q_heads=16, kv_heads=4, head_dim=128, page=64, seed=0):
+    """One layer: the prompts in one call each of append and attention, then `steps` decoding steps of all requests, the second of which ends
+    half-way and makes room for another.  Random activations stand for a model's.  Returns the relative error of the outputs against
+    attention over keys and values that were never quantized, for the prompts and for the steps."""
+    from . import binding as B
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    total = max(prompts) + steps + 1
+    seqs = Sequences(len(prompts), 2 * sum(-(-(n + steps) // page) + 1 for n in prompts), page, total)
+    cache = B.PagedCache(seqs.free_pages, kv_heads, head_dim, page)
+    cos, sin = rope_tables(total, head_dim)
+    past = [[torch.zeros(h, 0, head_dim, device="cuda") for _ in range(2)] for h in [kv_heads] * len(prompts)]
+    errors = {"prompt": [0.0, 0.0], "step": [0.0, 0.0]}
+
+    def turn(x, at):
+        c, s = cos[at:at + x.shape[-2]], sin[at:at + x.shape[-2]]
+        a, b = x.float().chunk(2, -1)
+        return torch.cat((a * c - b * s, b * c + a * s), -1)
+
+    def step(new, kind):
+        n = seqs.extend(new)
+        q, k, v = (torch.randn(len(prompts), h, n, head_dim, device="cuda", generator=g).bfloat16() for h in (q_heads, kv_heads, kv_heads))
+        B.kvq_paged_append(cache, k, v, seqs.page_table, seqs.lengths, n_new=seqs.n_new, cos=cos, sin=sin)
+        out = B.kvq_paged_attn(cache, q, seqs.page_table, seqs.lengths, head_dim ** -0.5, n_new=seqs.n_new, cos=cos, sin=sin)
+        for s, m in new.items():
+            at = past[s][0].shape[1]
+            past[s][0] = torch.cat((past[s][0], turn(k[s, :, :m], at)), 1)
+            past[s][1] = torch.cat((past[s][1], v[s, :, :m].float()), 1)
+            kk, vv = (x.repeat_interleave(q_heads // kv_heads, 0) for x in past[s])
+            w = turn(q[s, :, :m], at) @ kk.transpose(-1, -2) * head_dim ** -0.5
+            hidden = torch.arange(at + m, device="cuda") > at + torch.arange(m, device="cuda")[:, None]
+            want = torch.softmax(w.masked_fill(hidden, float("-inf")), -1) @ vv
+            errors[kind][0] += float((out[s, :, :m].float() - want).square().sum())
+            errors[kind][1] += float(want.square().sum())
+        seqs.commit()
+
+    step(dict(enumerate(prompts)), "prompt")
+    for i in range(steps):
+        if i == steps // 2 and len(prompts) > 1:
+            seqs.release(1)
+            past[1] = [x[:, :0] for x in past[1]]
+            step({1: prompts[1]}, "prompt")
+        step({s: 1 for s in range(len(prompts))}, "step")
+    return {k: (a / b) ** 0.5 for k, (a, b) in errors.items()}
+
+
+def _main():
+    """python -m paper_2605_26266_b200.paged: the rollout's errors as one JSON line."""
+    import json
+    print(json.dumps({"paged_rollout": rollout(), "data": "synthetic"}))
+
+
+if __name__ == "__main__":
+    _main()

@@ -98,3 +98,20 @@ def test_every_kernel_may_start_early_and_waits(b):
         for body in text.split("__global__ ")[1:]:
             wait, allow = body.find("wait_for_previous_grid();"), body.find("allow_next_grid();")
             assert 0 <= wait < allow, (name, body[:80])
+
+
+def test_a_site_code_names_one_wait(b):
+    """The codes of the kernels' waits are those that the header lists; faults of the lists are arguments', not time-outs."""
+    with open(os.path.join(ROOT, "include", "kvq.h")) as f:
+        header = f.read()
+    listed = header[header.index("Few rows: 601"):header.index("#define KVQ_PAGED_BAD_PAGE")]
+    codes = {int(c) for c in re.findall(r"\b[67]\d\d\b", listed)}
+    found = []
+    for name in ("attn_few.cu", "attn_chunk.cu"):
+        found += [int(c) for c in re.findall(r"cx\.wait\([^;]*?, (\d{3})\)", source(name))]
+    assert set(found) == codes
+    assert {c for c in found if found.count(c) > 1} <= {711}                  # the keys of a segment's first tile, and of the next ones
+    for word in (b.KVQ_PAGED_BAD_PAGE, b.KVQ_PAGED_BAD_POSITION, b.KVQ_PAGED_BAD_LENGTH):
+        assert b.kvq_status_word_result(word) == b.KVQ_ERR_INVALID_ARG
+    for word in codes:
+        assert b.kvq_status_word_result(word) == b.KVQ_ERR_TIMEOUT
