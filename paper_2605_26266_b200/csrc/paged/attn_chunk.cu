@@ -55,6 +55,10 @@ template <int D>
 struct Chunk {
   static constexpr int kTile = kTileKeys * D;                       // bytes of a tile of codes, and of a part of a query tile
   static constexpr int kKStages = 3, kRawStages = 2, kVStages = 2;
+  // Heads of 64 channels leave tensor memory for weights of their own: the next scores are computed as soon as a tile's are in registers, while its weights are.
+  // Of 128 channels the weights lie over the scores, which the next ones have to wait for.
+  static constexpr bool kAhead = D == 64;
+  static constexpr int kTmemO = 256, kTmemP = kAhead ? 384 : 0, kColsP = kAhead ? 64 : 128;      // columns; from one query tile's weights to the other's
   static constexpr int kOffQ = 0;                                   // [query tile][part]
   static constexpr int kOffK = kOffQ + 4 * kTile;
   static constexpr int kOffRaw = kOffK + kKStages * kTile;
@@ -62,7 +66,7 @@ struct Chunk {
   static constexpr int kOffBar = kOffV + kVStages * 2 * kTile;
   enum { kKFull = 0, kKEmpty = kKFull + kKStages, kRawFull = kKEmpty + kKStages, kRawEmpty = kRawFull + kRawStages, kVFull = kRawEmpty + kRawStages,
          kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPFull = kSFull + 2, kODone = kPFull + 4,      // of weights: + 2 half + query tile
-         kOFree = kODone + 2, kTurn = kOFree + 2, kDrain = kTurn + 2, kBars = kDrain + 2 };
+         kOFree = kODone + 2, kTurn = kOFree + 2, kSFree = kTurn + 2, kDrain = kSFree + 2, kBars = kDrain + 2 };
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kOffScale = (kOffMisc + 8 + 127) / 128 * 128;      // [8 tiles][3][8] floats: key factors, value exponents, their inverses
   static constexpr int kSmem = kOffScale + 8 * 96 + 1024;
@@ -129,55 +133,79 @@ struct Blocks {
   }
 };
 
-// One block: the line of steps (sequence, key head, row block, tile), cut evenly.
+// One block of kRows threads: the line of steps (sequence, key head, row block, tile), cut evenly.  The chunk kernel waits for it, so that what counts is its
+// latency: lengths are read once and sums stay in shared memory where a thread has one sequence at most, and divisions are 32 bits wide where that does.
 __device__ void make_schedule(const ChunkParams& p, int ctas) {
-  __shared__ long long s_sum[kRows];
-  const int tid = threadIdx.x;
+  __shared__ long long s_upto[kRows], s_warp[kRows / 32];
+  __shared__ Extent s_ex[kRows];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool small = p.seqs.batch <= kRows;
   long long before = 0;
   for (int b0 = 0; b0 < p.seqs.batch; b0 += kRows) {
     const int b = b0 + tid;
-    long long mine = 0;
+    long long upto = 0;
     if (b < p.seqs.batch) {
       const Extent ex = extent_of(p.seqs, p.pool.page, b, p.m_tokens, nullptr);
+      s_ex[tid] = ex;
       const int blocks = blocks_of(ex, p.group);
       if (p.causal) {
         Blocks it(ex, p.group);
-        for (int rb = 0; rb < blocks; ++rb) mine += it.next(ex, p) + kUnitSteps;
+        for (int rb = 0; rb < blocks; ++rb) upto += it.next(ex, p) + kUnitSteps;
       } else {
-        mine = (long long)blocks * (tiles_of(ex, 0, 1, 0, 0).count + kUnitSteps);
+        upto = (long long)blocks * (tiles_of(ex, 0, 1, 0, 0).count + kUnitSteps);
       }
+      upto *= p.pool.kv_heads;
     }
-    s_sum[tid] = mine * p.pool.kv_heads;
+#pragma unroll
+    for (int i = 1; i < 32; i <<= 1) {
+      const long long add = __shfl_up_sync(0xFFFFFFFFu, upto, i);
+      if (lane >= i) upto += add;
+    }
+    if (lane == 31) s_warp[warp] = upto;
     __syncthreads();
-    for (int i = 1; i < kRows; i <<= 1) {
-      const long long add = tid >= i ? s_sum[tid - i] : 0;
-      __syncthreads();
-      s_sum[tid] += add;
-      __syncthreads();
+    long long sum = 0;
+#pragma unroll
+    for (int i = 0; i < kRows / 32; ++i) {
+      if (i < warp) upto += s_warp[i];
+      sum += s_warp[i];
     }
-    if (b < p.seqs.batch) p.upto[b] = before + s_sum[tid];
-    before += s_sum[kRows - 1];
+    upto += before;
+    before += sum;
+    s_upto[tid] = upto;
+    if (!small && b < p.seqs.batch) p.upto[b] = upto;
     __syncthreads();
   }
-  const long long all = before, n = min((long long)ctas, all);      // no range between two others is empty
+  auto upto_of = [&](int b) { return small ? s_upto[b] : load_coherent(p.upto + b); };
+  const long long all = before;
+  const int n = (int)min((long long)ctas, all);                  // no range between two others is empty
+  auto cut = [&](int i) { return all < 1 << 22 ? (long long)((uint32_t)all * (uint32_t)i / (uint32_t)n) : all * i / n; };      // at most 1024 CTAs
   for (int c = tid; c < ctas; c += kRows) {
     Place r{0, 0, 0, 0, 0};
     if (c < n) {
-      const long long lo = all * c / n;
-      r.left = all * (c + 1) / n - lo;
+      const long long lo = cut(c);
+      r.left = cut(c + 1) - lo;
       int first = 0, last = p.seqs.batch - 1;                   // the first sequence with more than lo up to its end
       while (first < last) {
         const int mid = (first + last) >> 1;
-        if (load_coherent(p.upto + mid) > lo) last = mid; else first = mid + 1;
+        if (upto_of(mid) > lo) last = mid; else first = mid + 1;
       }
-      const long long start = first ? load_coherent(p.upto + first - 1) : 0, per = (load_coherent(p.upto + first) - start) / p.pool.kv_heads;
+      const long long start = first ? upto_of(first - 1) : 0, mine = upto_of(first) - start, in_seq = lo - start;
+      const Extent ex = small ? s_ex[first] : extent_of(p.seqs, p.pool.page, first, p.m_tokens, nullptr);
+      long long in;
       r.b = first;
-      r.h = (int)((lo - start) / per);
-      long long in = (lo - start) % per;
-      const Extent ex = extent_of(p.seqs, p.pool.page, r.b, p.m_tokens, nullptr);
+      if (mine < 1ll << 31) {
+        const uint32_t per = (uint32_t)mine / (uint32_t)p.pool.kv_heads;
+        r.h = (int)((uint32_t)in_seq / per);
+        in = (uint32_t)in_seq % per;
+      } else {
+        const long long per = mine / p.pool.kv_heads;
+        r.h = (int)(in_seq / per);
+        in = in_seq % per;
+      }
       Blocks it(ex, p.group);
+      const int same = tiles_of(ex, 0, 1, 0, 0).count;
       for (;; ++r.rb) {
-        const int count = (p.causal ? it.next(ex, p) : tiles_of(ex, 0, 1, 0, 0).count) + kUnitSteps;
+        const int count = (p.causal ? it.next(ex, p) : same) + kUnitSteps;
         if (in < count) break;
         in -= count;
       }
@@ -334,6 +362,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       mbar_init(cx.bar(F::kVFull + s), 128); mbar_init(cx.bar(F::kVEmpty + s), 2);
       mbar_init(cx.bar(F::kQFull + s), 1); mbar_init(cx.bar(F::kOFree + s), 128);
       mbar_init(cx.bar(F::kSFull + s), 1); mbar_init(cx.bar(F::kODone + s), 1); mbar_init(cx.bar(F::kTurn + s), 1); mbar_init(cx.bar(F::kDrain + s), 1);
+      mbar_init(cx.bar(F::kSFree + s), 128);
       mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kPFull + 2 + s), 128);
     }
     mbar_init(cx.bar(F::kQEmpty), 2);
@@ -350,7 +379,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + F::kOffMisc);
   const int4 at = load_coherent(p.places + 2 * blockIdx.x), left = load_coherent(p.places + 2 * blockIdx.x + 1);
   const Place place{at.x, at.y, at.z, at.w, (long long)(uint32_t)left.x | (long long)left.y << 32};
-  // TMEM columns: S0 [0,128) S1 [128,256) O0 [256, 256 + D) O1 [384, 384 + D); weights (FP16 pairs) over the first 64 columns of their scores.
+  // TMEM columns: S0 [0, 128), S1 [128, 256), O0 and O1 from 256; weights (FP16 pairs) over the first 64 columns of their scores, or of 64 channels from 384.
 
   if (warp < 4) {
     setmaxnreg_dec<kRegsIssue>();
@@ -429,7 +458,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const uint64_t dq = make_smem_desc(sbase + F::kOffQ + qt * 2 * F::kTile, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
       const uint64_t dk = make_smem_desc(sbase + F::kOffK, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
       const uint64_t dv = make_smem_desc(sbase + F::kOffV, kTileKeys * 128, 1024, kLayoutSw128);
-      const uint32_t s_tmem = tmem + qt * 128, o_tmem = tmem + 256 + qt * 128;
+      const uint32_t s_tmem = tmem + qt * 128, o_tmem = tmem + F::kTmemO + qt * D, p_tmem = tmem + F::kTmemP + qt * F::kColsP;
       Walker w(place);
       Segment sg;
       int it = 0, n = 0, nseg = 0, nact = 0, turns = 0;        // tiles, tiles and segments of this query tile, its turns
@@ -448,19 +477,19 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         if (!leader) return;
 #pragma unroll
         for (int k = 0; k < 4; ++k)                            // 16 keys a step
-          mma_ts(o_tmem, s_tmem + 32 * hf + 8 * k, dv + (uint64_t)((s * 2 * F::kTile + (4 * hf + k) * 16 * 128) >> 4), idesc_o, add || k > 0);
+          mma_ts(o_tmem, p_tmem + 32 * hf + 8 * k, dv + (uint64_t)((s * 2 * F::kTile + (4 * hf + k) * 16 * 128) >> 4), idesc_o, add || k > 0);
       };
       // The two query tiles take turns at the tensor pipe: O += P V of one and at once its next scores, then the same of the other.  That keeps the softmax groups
       // half a step apart: one has its exponentials while the other waits for products.  Each has its own warp, whose waits and commits then do not hold up
       // the other's products.
       auto my_turn = [&](bool both) -> bool {
-        if (!both) return true;
+        if (F::kAhead || !both) return true;
         const bool r = all_lanes(cx.wait(F::kTurn + qt, (turns & 1) ^ 1 ^ qt, 716));
         ++turns;
         return r;
       };
       auto pass_on = [&](bool both) {
-        if (both && leader) mbar_arrive(cx.bar(F::kTurn + (qt ^ 1)));
+        if (!F::kAhead && both && leader) mbar_arrive(cx.bar(F::kTurn + (qt ^ 1)));
         __syncwarp();
       };
       while (ok && w.next(sg, p)) {
@@ -479,8 +508,20 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         for (int t = sg.tb; t < sg.te; ++t, ++it) {
           const int vs = it & 1, s1 = (it + 1) % F::kKStages;
           const bool next = t + 1 < sg.te;
-          if (!(ok = all_lanes(cx.wait(F::kVFull + vs, it >> 1 & 1, 713)))) break;
           if (next && !(ok = all_lanes(cx.wait(F::kKFull + s1, (it + 1) / F::kKStages & 1, 711)))) break;
+          if (F::kAhead && next) {
+            if (act) {
+              if (!(ok = all_lanes(cx.wait(F::kSFree + qt, n & 1, 718)))) break;
+              tc_fence_after();
+              scores(it + 1);
+            }
+            if (leader) {
+              tc_commit(cx.bar(F::kKEmpty + s1));
+              if (t + 2 == sg.te) tc_commit(cx.bar(F::kQEmpty));
+            }
+            __syncwarp();
+          }
+          if (!(ok = all_lanes(cx.wait(F::kVFull + vs, it >> 1 & 1, 713)))) break;
           if (act) {
             if (t == sg.tb && !(ok = all_lanes(cx.wait(F::kOFree + qt, (nact & 1) ^ 1, 714)))) break;
             if (!(ok = all_lanes(cx.wait(F::kPFull + qt, n & 1, 715)))) break;
@@ -490,15 +531,15 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             if (!(ok = all_lanes(cx.wait(F::kPFull + 2 + qt, n & 1, 717)))) break;
             tc_fence_after();
             products(vs, 1, true);
-            if (leader && !next) tc_commit(cx.bar(F::kODone + qt));
-            if (next) scores(it + 1);
+            if (leader && (F::kAhead || !next)) tc_commit(cx.bar(F::kODone + qt));
+            if (!F::kAhead && next) scores(it + 1);
             pass_on(both);
             ++n;
           }
           if (leader) {
             tc_commit(cx.bar(F::kVEmpty + vs));
-            if (next) tc_commit(cx.bar(F::kKEmpty + s1));
-            if (t + 2 == sg.te) tc_commit(cx.bar(F::kQEmpty));
+            if (!F::kAhead && next) tc_commit(cx.bar(F::kKEmpty + s1));
+            if (!F::kAhead && t + 2 == sg.te) tc_commit(cx.bar(F::kQEmpty));
           }
           __syncwarp();
         }
@@ -513,7 +554,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       if (ok) {
         for (int k = max(it - F::kKStages, 0); k < it; ++k) cx.drain(F::kKEmpty + k % F::kKStages, k / F::kKStages & 1);
         for (int k = max(it - 2, 0); k < it; ++k) cx.drain(F::kVEmpty + (k & 1), k >> 1 & 1);
-        if (n > 0) { cx.drain(F::kSFull + qt, (n - 1) & 1); cx.drain(F::kODone + qt, (nact - 1) & 1); }
+        if (n > 0) { cx.drain(F::kSFull + qt, (n - 1) & 1); cx.drain(F::kODone + qt, ((F::kAhead ? n : nact) - 1) & 1); }
         if (nseg > 0) cx.drain(F::kQEmpty, (nseg - 1) & 1);
       }
     } else if (warp == 3) {
@@ -543,7 +584,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const int qt = (warp - 4) >> 2, wq = warp & 3;
     const int r256 = qt * 128 + wq * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
-    const uint32_t s_addr = tmem + lane_addr + qt * 128, o_addr = tmem + lane_addr + 256 + qt * 128;
+    const uint32_t s_addr = tmem + lane_addr + qt * 128, o_addr = tmem + lane_addr + F::kTmemO + qt * D, p_addr = tmem + lane_addr + F::kTmemP + qt * F::kColsP;
     int4* header = p.headers + 2 * blockIdx.x;
     if (tid == 128) header[0] = header[1] = make_int4(kNone, 0, 0, 0);
     Walker w(place);
@@ -580,6 +621,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           v[4 * h] = v4.x; v[4 * h + 1] = v4.y; v[4 * h + 2] = v4.z; v[4 * h + 3] = v4.w;
         }
         tmem_wait_ld();
+        if (F::kAhead) {
+          tc_fence_before();
+          mbar_arrive(cx.bar(F::kSFree + qt));
+        }
         if (edge) {
           const int nv = min(hi, total) - first, nl = lo - first;
 #pragma unroll
@@ -595,7 +640,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           m_new = fmaxf(m_new, fmaf(max3(a, b, fmaxf(c, at(15))), f[i], v[i]));
         }
         if (__any_sync(0xFFFFFFFFu, m_new - m > kSlack)) {
-          if (t > sg.tb) {                             // the last product on O is done: the commit of these scores came after it
+          if (t > sg.tb) {
+            if (F::kAhead) {                           // the last product on O; of 128 channels these scores' commit came after it
+              ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 722));
+              if (!ok) break;
+              tc_fence_after();
+            }
             const float drop = ex2(m - m_new);
 #pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
@@ -628,21 +678,29 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             s[k / 2] = cvt_f16x2(w2.x, w2.y);
           }
           l = fmaf(sum.x + sum.y, inv[i], l);
-          if (i == 3) st32_plain(s_addr, s);
+          if (i == 3) {
+            if (F::kAhead && t > sg.tb) {              // the last product has read the weights before
+              ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 724));
+              if (!ok) break;
+              tc_fence_after();
+            }
+            st32_plain(p_addr, s);
+          }
           if (i == 5) {
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(cx.bar(F::kPFull + qt));
           }
         }
-        tmem_st32(s_addr + 32, s + 32);
+        if (!ok) break;
+        tmem_st32(p_addr + 32, s + 32);
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(cx.bar(F::kPFull + 2 + qt));
       }
       if (!ok) break;
       // ---- the rows' results ----
-      ok = all_lanes(cx.wait(F::kODone + qt, nact & 1, 723));            // the segment's last product
+      ok = all_lanes(cx.wait(F::kODone + qt, (F::kAhead ? n - 1 : nact) & 1, 723));      // the segment's last product
       if (!ok) break;
       tc_fence_after();
       if (!(rowf == rowf)) l = rowf;                             // a query that is no finite number
@@ -744,25 +802,30 @@ __global__ void __launch_bounds__(256) paged_chunk_merge_kernel(const ChunkParam
   using F = Chunk<D>;
   wait_for_previous_grid();
   allow_next_grid();
-  const int c = blockIdx.x, r = blockIdx.y * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
-  int slot = 0;
-  int4 hd = load_coherent(p.headers + 2 * c);
-  if ((hd.x & 3) != kStart) { hd = load_coherent(p.headers + 2 * c + 1); slot = 1; }
+  const int c = blockIdx.x, lane = threadIdx.x & 31, r = blockIdx.y * 32 + lane, warp = threadIdx.x >> 5;
+  const int4 h0 = load_coherent(p.headers + 2 * c), h1 = load_coherent(p.headers + 2 * c + 1);
+  const int slot = (h0.x & 3) == kStart ? 0 : 1;
+  const int4 hd = slot ? h1 : h0;
   const int row = hd.z * kRows + r, tok = row / p.group, g = row - tok * p.group;
-  if ((hd.x & 3) != kStart || tok >= hd.w) return;
+  if ((hd.x & 3) != kStart || (hd.z * kRows + (int)blockIdx.y * 32) / p.group >= hd.w) return;      // the same for the block
+  // the last CTA that worked on the unit: 32 headers at a time
+  int end = ctas;
+  for (int k0 = c + 1; k0 < end; k0 += 32) {
+    const bool last = k0 + lane < ctas && (load_coherent(p.headers + 2 * (k0 + lane)).x & 3) != kMiddle;
+    const unsigned ends = __ballot_sync(0xFFFFFFFFu, last);
+    if (ends) end = k0 + __ffs(ends);
+  }
+  if (tok >= hd.w) return;
+  auto slot_of = [&](int k) { return p.slots + (size_t)(2 * k + (k == c ? slot : 0)) * F::kSlotBytes; };
   const int head = (hd.x >> 2) * p.group + g;
   float m = -INFINITY;
-  int end = c;
-  for (int k = c; k < ctas; ++k) {
-    const uint8_t* from = p.slots + (size_t)(2 * k + (k == c ? slot : 0)) * F::kSlotBytes;
-    m = fmaxf(m, load_coherent(reinterpret_cast<const float*>(from + F::kSlotStats) + r));
-    end = k;
-    if (k > c && (load_coherent(p.headers + 2 * k).x & 3) != kMiddle) break;
-  }
+#pragma unroll 4
+  for (int k = c; k < end; ++k) m = fmaxf(m, load_coherent(reinterpret_cast<const float*>(slot_of(k) + F::kSlotStats) + r));
   float l = 0.f;
   float4 o[D / 32] = {};
-  for (int k = c; k <= end; ++k) {
-    const uint8_t* from = p.slots + (size_t)(2 * k + (k == c ? slot : 0)) * F::kSlotBytes;
+#pragma unroll 2
+  for (int k = c; k < end; ++k) {
+    const uint8_t* from = slot_of(k);
     const float* st = reinterpret_cast<const float*>(from + F::kSlotStats);
     const float a = ex2(load_coherent(st + r) - m);
     l = fmaf(load_coherent(st + kRows + r), a, l);
