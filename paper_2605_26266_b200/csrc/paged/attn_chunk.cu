@@ -628,8 +628,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         if (edge) {
           const int nv = min(hi, total) - first, nl = lo - first;
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i >= nv || i < nl) s[i] = 0xFF800000u;
+          for (int c = 0; c < 128; c += 32)                      // most of an edge tile's pieces are seen whole by all rows of the warp
+            if (!__all_sync(0xFFFFFFFFu, c + 32 <= nv && c >= nl)) {
+#pragma unroll
+              for (int i = c; i < c + 32; ++i)
+                if (i >= nv || i < nl) s[i] = 0xFF800000u;
+            }
         }
         float m_new = m;
 #pragma unroll
