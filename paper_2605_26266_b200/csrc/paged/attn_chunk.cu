@@ -12,7 +12,7 @@
 //   x = f s + b - m + 4,   P = 2^x,   l += 2^(x - b),   out = sum P code / l
 // The running maximum m is raised, and O scaled, only when it has grown by more than 8, so P <= 2^12.
 //
-// Work: the tile steps of all units in one line, cut evenly over the CTAs (lengths are on the device: every CTA finds its place itself).  Units that
+// Work: the tile steps of all units in one line, cut evenly over the CTAs (lengths are on the device, and so is the cut: one block of the kernel ahead makes it).  Units that
 // are cut leave FP32 partial rows for the merge kernel.
 #include "tensor.cuh"
 
@@ -54,7 +54,7 @@ enum { kNone = 0, kStart = 1, kMiddle = 2, kEnd = 3 };
 template <int D>
 struct Chunk {
   static constexpr int kTile = kTileKeys * D;                       // bytes of a tile of codes, and of a part of a query tile
-  static constexpr int kKStages = 3, kRawStages = 2, kVStages = 2;
+  static constexpr int kKStages = 3, kRawStages = 2, kVStages = 2, kSegs = 4;
   // Heads of 64 channels leave tensor memory for weights of their own: the next scores are computed as soon as a tile's are in registers, while its weights are.
   // Of 128 channels the weights lie over the scores, which the next ones have to wait for.
   static constexpr bool kAhead = D == 64;
@@ -66,10 +66,13 @@ struct Chunk {
   static constexpr int kOffBar = kOffV + kVStages * 2 * kTile;
   enum { kKFull = 0, kKEmpty = kKFull + kKStages, kRawFull = kKEmpty + kKStages, kRawEmpty = kRawFull + kRawStages, kVFull = kRawEmpty + kRawStages,
          kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPFull = kSFull + 2, kODone = kPFull + 4,      // of weights: + 2 half + query tile
-         kOFree = kODone + 2, kTurn = kOFree + 2, kSFree = kTurn + 2, kDrain = kSFree + 2, kBars = kDrain + 2 };
+         kOFree = kODone + 2, kTurn = kOFree + 2, kSFree = kTurn + 2, kSegFull = kSFree + 2,
+         kSegEmpty = kSegFull + kSegs, kDrain = kSegEmpty + kSegs, kBars = kDrain + 2 };
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kOffScale = (kOffMisc + 8 + 127) / 128 * 128;      // [8 tiles][3][8] floats: key factors, value exponents, their inverses
-  static constexpr int kSmem = kOffScale + 8 * 96 + 1024;
+  static constexpr int kOffSeg = kOffScale + 8 * 96;                 // [segments][16] ints
+  static constexpr int kOffRow = kOffSeg + kSegs * 64;               // [segments][256] floats: factors of the rows
+  static constexpr int kSmem = kOffRow + kSegs * kRows * 4 + 1024;
   static constexpr int kSlotStats = kRows * D * 4;
   static constexpr int kSlotBytes = kSlotStats + 2 * kRows * 4;
 };
@@ -118,6 +121,30 @@ struct Walker {
     at.behind = 0;
     ++at.rb;
     return s.te > s.tb;                                         // a range may end in a unit's start
+  }
+};
+
+// What a CTA works on next, from the ring that the query warp fills: lengths, divisions and the line's order are its business alone (each role's own walk took
+// 2 000 to 3 500 cycles between two units).  A warp reads together.
+template <int D>
+struct Reader {
+  const Waits& cx;
+  const uint8_t* smem;
+  int n;
+  __device__ __forceinline__ Reader(const Waits& c, const uint8_t* s) : cx(c), smem(s), n(0) {}
+  // row: which factor of the unit's rows goes to *factor (nullptr: none)
+  __device__ __forceinline__ bool next(Segment& s, int row = 0, float* factor = nullptr) {
+    using F = Chunk<D>;
+    const int slot = n % F::kSegs;
+    if (!__all_sync(0xFFFFFFFFu, cx.wait(F::kSegFull + slot, n / F::kSegs & 1, 741))) return false;
+    const int4* at = reinterpret_cast<const int4*>(smem + F::kOffSeg + slot * 64);
+    const int4 a = at[0], b = at[1], c = at[2];
+    s.b = a.x; s.h = a.y; s.rb = a.z; s.tb = a.w; s.te = b.x; s.n = b.y; s.first = b.z; s.ex = Extent{b.w, c.x};
+    if (factor) *factor = reinterpret_cast<const float*>(smem + F::kOffRow)[slot * kRows + row];
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(cx.bar(F::kSegEmpty + slot));
+    ++n;
+    return s.b >= 0;
   }
 };
 
@@ -366,6 +393,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kPFull + 2 + s), 128);
     }
     mbar_init(cx.bar(F::kQEmpty), 2);
+    for (int s = 0; s < F::kSegs; ++s) { mbar_init(cx.bar(F::kSegFull + s), 1); mbar_init(cx.bar(F::kSegEmpty + s), 15); }      // all warps but the query warp
     fence_barrier_init();
     prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
   }
@@ -386,11 +414,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     if (warp == 0) {
       // ================= producer =================
       const int ppt = kTileKeys >> p.pool.log2_page;           // pages of a tile
-      Walker w(place);
+      Reader<D> w(cx, smem);
       Segment sg;
       int it = 0, raws = 0;
       bool ok = true;
-      while (ok && w.next(sg, p)) {
+      while (ok && w.next(sg)) {
         const int32_t* table = p.seqs.table + (int64_t)sg.b * p.seqs.table_stride;
         const int last = (sg.ex.before + sg.ex.fresh - 1) >> p.pool.log2_page;
         // 32 pages at a time, a page a lane, a batch ahead; one past the pool's end where there is none: the copy brings zeros, and scale byte 255 hides them
@@ -459,7 +487,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const uint64_t dk = make_smem_desc(sbase + F::kOffK, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
       const uint64_t dv = make_smem_desc(sbase + F::kOffV, kTileKeys * 128, 1024, kLayoutSw128);
       const uint32_t s_tmem = tmem + qt * 128, o_tmem = tmem + F::kTmemO + qt * D, p_tmem = tmem + F::kTmemP + qt * F::kColsP;
-      Walker w(place);
+      Reader<D> w(cx, smem);
       Segment sg;
       int it = 0, n = 0, nseg = 0, nact = 0, turns = 0;        // tiles, tiles and segments of this query tile, its turns
       bool ok = true;
@@ -492,7 +520,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         if (!F::kAhead && both && leader) mbar_arrive(cx.bar(F::kTurn + (qt ^ 1)));
         __syncwarp();
       };
-      while (ok && w.next(sg, p)) {
+      while (ok && w.next(sg)) {
         const int rows = sg.ex.fresh * p.group - sg.rb * kRows;
         const bool act = rows > qt * 128, both = rows > 128;
         if (!(ok = all_lanes(cx.wait(F::kQFull + qt, nseg & 1, 712)) && all_lanes(cx.wait(F::kKFull + it % F::kKStages, it / F::kKStages & 1, 711)))) break;
@@ -558,25 +586,53 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         if (nseg > 0) cx.drain(F::kQEmpty, (nseg - 1) & 1);
       }
     } else if (warp == 3) {
-      // ================= queries =================
+      // ================= units in order, and their queries =================
       Walker w(place);
-      Segment sg;
-      int nseg = 0;
-      while (w.next(sg, p)) {
-        if (!all_lanes(cx.wait(F::kQEmpty, (nseg & 1) ^ 1, 703))) break;      // the scores of the segment before are done
-        if (lane == 0) {
-          const int64_t unit = ((int64_t)sg.b * p.pool.kv_heads + sg.h) * p.max_blocks + sg.rb;
-#pragma unroll
-          for (int qt = 0; qt < 2; ++qt) {
-            mbar_arrive_expect_tx(cx.bar(F::kQFull + qt), 2 * F::kTile);
-            bulk_load(sbase + F::kOffQ + qt * 2 * F::kTile, p.queries + (unit * 2 + qt) * (2 * F::kTile), 2 * F::kTile, cx.bar(F::kQFull + qt));
+      Segment sg, before;
+      bool more = true;
+      int loaded = 0, announced = 0;
+      // unit n is announced, with its rows' factors, before the queries of unit n - 1 are waited for
+      for (int n = 0;; ++n) {
+        if (more) {
+          more = w.next(sg, p);
+          const int slot = n % F::kSegs;
+          if (!all_lanes(cx.wait(F::kSegEmpty + slot, (n / F::kSegs & 1) ^ 1, 742))) break;
+          if (lane == 0) {
+            int4* at = reinterpret_cast<int4*>(smem + F::kOffSeg + slot * 64);
+            at[0] = make_int4(more ? sg.b : -1, sg.h, sg.rb, sg.tb);
+            at[1] = make_int4(sg.te, sg.n, sg.first, sg.ex.before);
+            at[2] = make_int4(sg.ex.fresh, 0, 0, 0);
+            if (more) {
+              mbar_arrive_expect_tx(cx.bar(F::kSegFull + slot), kRows * 4);
+              bulk_load(sbase + F::kOffRow + slot * kRows * 4, p.factors + (((int64_t)sg.b * p.pool.kv_heads + sg.h) * p.max_blocks + sg.rb) * kRows, kRows * 4,
+                        cx.bar(F::kSegFull + slot));
+            } else {
+              mbar_arrive(cx.bar(F::kSegFull + slot));
+            }
           }
+          __syncwarp();
+          announced = n + 1;
         }
-        __syncwarp();
-        ++nseg;
+        if (n > 0) {
+          if (!all_lanes(cx.wait(F::kQEmpty, ((n - 1) & 1) ^ 1, 703))) break;      // the scores of the unit before are done
+          if (lane == 0) {
+            const int64_t unit = ((int64_t)before.b * p.pool.kv_heads + before.h) * p.max_blocks + before.rb;
+#pragma unroll
+            for (int qt = 0; qt < 2; ++qt) {
+              mbar_arrive_expect_tx(cx.bar(F::kQFull + qt), 2 * F::kTile);
+              bulk_load(sbase + F::kOffQ + qt * 2 * F::kTile, p.queries + (unit * 2 + qt) * (2 * F::kTile), 2 * F::kTile, cx.bar(F::kQFull + qt));
+            }
+          }
+          __syncwarp();
+          loaded = n;
+        }
+        if (!more) break;
+        before = sg;
       }
-      if (*cx.abort && nseg > 0)
-        for (int qt = 0; qt < 2; ++qt) cx.drain(F::kQFull + qt, (nseg - 1) & 1);
+      if (*cx.abort) {                                         // what is in flight lands before the CTA goes
+        for (int qt = 0; qt < 2 && loaded > 0; ++qt) cx.drain(F::kQFull + qt, (loaded - 1) & 1);
+        for (int k = max(announced - F::kSegs, 0); k < announced; ++k) cx.drain(F::kSegFull + k % F::kSegs, k / F::kSegs & 1);
+      }
     }
   } else if (warp < 12) {
     // ================= softmax: a query row a thread =================
@@ -587,11 +643,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const uint32_t s_addr = tmem + lane_addr + qt * 128, o_addr = tmem + lane_addr + F::kTmemO + qt * D, p_addr = tmem + lane_addr + F::kTmemP + qt * F::kColsP;
     int4* header = p.headers + 2 * blockIdx.x;
     if (tid == 128) header[0] = header[1] = make_int4(kNone, 0, 0, 0);
-    Walker w(place);
+    Reader<D> w(cx, smem);
     Segment sg;
     int it = 0, n = 0, nseg = 0, nact = 0;
+    float rowf;                                                      // factor of this row's scores
     bool ok = true;
-    while (ok && w.next(sg, p)) {
+    while (ok && w.next(sg, r256, &rowf)) {
       const int rows = sg.ex.fresh * p.group - sg.rb * kRows;        // of this block and after it
       if (rows <= qt * 128) { it += sg.te - sg.tb; ++nseg; continue; }
       const int total = sg.ex.before + sg.ex.fresh;
@@ -600,7 +657,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const int pos = sg.ex.before + tok;
       const int hi = real ? (p.causal ? pos + 1 : total) : 0x7FFFFFFF, lo = real && p.window ? pos + 1 - p.window : 0;      // keys [lo, hi) are seen
       float m = kNoMax, l = 0.f;
-      const float rowf = load_coherent(p.factors + (((int64_t)sg.b * p.pool.kv_heads + sg.h) * p.max_blocks + sg.rb) * kRows + r256);
 #pragma unroll 1
       for (int t = sg.tb; t < sg.te; ++t, ++it, ++n) {
         ok = all_lanes(cx.wait(F::kSFull + qt, n & 1, 721));
@@ -762,11 +818,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     // ================= expanding warps: values of a tile to FP16 =================
     setmaxnreg_dec<kRegsExpand>();
     const int dt = tid - 384;
-    Walker w(place);
+    Reader<D> w(cx, smem);
     Segment sg;
     int it = 0;
     bool ok = true;
-    while (ok && w.next(sg, p)) {
+    while (ok && w.next(sg)) {
       for (int t = sg.tb; t < sg.te; ++t, ++it) {
         const int s = it & 1;
         ok = all_lanes(cx.wait(F::kRawFull + s, it >> 1 & 1, 732));

@@ -9,7 +9,7 @@ from tests import paged_testlib as P
 pytestmark = pytest.mark.gpu
 
 SITE_CODES = {601, 611, 612, 613, 614, 621, 622, 623, 624, 625, 631,
-              701, 702, 703, 711, 712, 713, 714, 715, 716, 717, 718, 721, 722, 723, 724, 732, 733}
+              701, 702, 703, 711, 712, 713, 714, 715, 716, 717, 718, 721, 722, 723, 724, 732, 733, 741, 742}
 
 
 @pytest.fixture(scope="module")
