@@ -35,6 +35,7 @@ struct FewParams {
   int32_t* status;
   uint8_t* slots;                  // partial rows
   int4* headers;                   // [CTAs][2]: what a slot holds
+  int whole;                       // a CTA for each unit
   uint32_t wait_budget;
 };
 
@@ -97,6 +98,14 @@ struct Walker {
 // One warp: the place of CTA c of n in the line.  Lengths are read once where a lane has one sequence at most.
 __device__ __forceinline__ Place find_place(const FewParams& p, int c, int n) {
   const int lane = threadIdx.x & 31;
+  if (p.whole) {
+    Place r{};
+    r.b = c / p.pool.kv_heads; r.h = c - r.b * p.pool.kv_heads;
+    r.ex = extent_of(p.seqs, p.pool.page, r.b, p.m_tokens, p.status);
+    r.tl = tiles_of(r.ex, 0, p.m_tokens, p.causal, p.window);
+    r.left = r.tl.count;
+    return r;
+  }
   auto extent_at = [&](int b, int32_t* status) { return b < p.seqs.batch ? extent_of(p.seqs, p.pool.page, b, p.m_tokens, status) : Extent{0, 0}; };
   auto tiles_at = [&](const Extent& ex) { return (long long)tiles_of(ex, 0, p.m_tokens, p.causal, p.window).count * p.pool.kv_heads; };
   const Extent ex0 = extent_at(lane, p.status);
@@ -445,10 +454,12 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         // keys that a row does not see; whole tiles that all rows see need no test
         const int tile0 = (sg.first + t) * kTileKeys, seen = p.causal ? sg.ex.before + 1 : total;      // what the first row sees
         if (tile0 + kTileKeys > seen || (p.window && tile0 <= sg.ex.before + sg.ex.fresh - 1 - p.window) || __any_sync(0xFFFFFFFFu, !there)) {
+          int at = sg.ex.before, g = 0;                             // the row's place in the sequence, without a division each
+          const int back = p.window ? p.window : 0x7FFFFFFF;
 #pragma unroll
           for (int r = 0; r < NR; ++r) {
-            const int at = sg.ex.before + r / p.group;
-            if (!there || (p.causal && j > at) || (p.window && j <= at - p.window)) x[r] = -INFINITY;
+            if (!there || (p.causal && j > at) || at - j >= back) x[r] = -INFINITY;
+            if (++g == p.group) { g = 0; ++at; }
           }
         }
         bool over = false;
@@ -534,7 +545,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         }
 #pragma unroll
         for (int i = kPer / 2; i; i >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
-        if (key % kPer == 0) part[key / kPer] = sum;
+        if (key % kPer == 0) { part[key / kPer] = sum; drop[key / kPer] = sum == 0.f ? 0.f : 1.f / sum; }
         named_barrier_sync(1, 128);
       }
       tc_fence_after();
@@ -550,21 +561,28 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       const int slot = nseg == 0 ? 0 : 1;
       float* to = whole ? nullptr : reinterpret_cast<float*>(p.slots + (size_t)(2 * blockIdx.x + slot) * F::kSlotBytes);
       if (!whole && key == 0) header[slot] = make_int4(sg.tb == 0 ? kStart : sg.te == sg.n ? kEnd : kMiddle, sg.b, sg.h, sg.ex.fresh);
-      uint16_t* out = p.out + (int64_t)sg.b * p.os.b + (int64_t)sg.h * p.group * p.os.h + key;
-      float* lse = p.lse ? p.lse + ((int64_t)sg.b * p.q_heads + sg.h * p.group) * p.m_tokens : nullptr;
-      int t = 0, g = 0;                                             // of row r
+      const int used = min(rows, sg.ex.fresh * p.group);            // rows of real queries
+      const int rt = key / p.group, rg = key - rt * p.group;        // of row `key`
+      if (whole) {
+        // through shared memory, so that a store is 16 bytes of a row
+        uint16_t* lines = reinterpret_cast<uint16_t*>(smem + F::kOffP);
 #pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        if (r >= rows || t >= sg.ex.fresh) break;
-        const float sum = part[r];
-        if (whole) {
-          if (key < D) out[(int64_t)g * p.os.h + (int64_t)t * p.os.t] = (uint16_t)f32_to_bf16_bits(sum == 0.f ? 0.f : __fdividef(o[r], sum));
-          if (lse && key == 0) lse[(int64_t)g * p.m_tokens + t] = (log2f(sum) - shift[r]) * 0.6931471805599453f;
-        } else {
-          if (key < D) to[r * D + key] = o[r];
-          if (key == 0) { to[NR * D + r] = -shift[r]; to[NR * D + NR + r] = sum; }
+        for (int r = 0; r < NR; ++r)
+          if (key < D) lines[r * D + key] = (uint16_t)f32_to_bf16_bits(o[r] * drop[r]);
+        named_barrier_sync(1, 128);
+        uint16_t* out = p.out + (int64_t)sg.b * p.os.b + (int64_t)sg.h * p.group * p.os.h;
+#pragma unroll 1
+        for (int i = key; i < used * (D / 8); i += 128) {
+          const int r = i / (D / 8), t = r / p.group, g = r - t * p.group;
+          *reinterpret_cast<uint4*>(out + (int64_t)g * p.os.h + (int64_t)t * p.os.t + 8 * (i % (D / 8))) = reinterpret_cast<const uint4*>(lines)[i];
         }
-        if (++g == p.group) { g = 0; ++t; }
+        if (p.lse && key < used)
+          p.lse[((int64_t)sg.b * p.q_heads + sg.h * p.group + rg) * p.m_tokens + rt] = (log2f(part[key]) - shift[key]) * 0.6931471805599453f;
+      } else {
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+          if (key < D && r < used) to[r * D + key] = o[r];
+        if (key < used) { to[NR * D + key] = -shift[key]; to[NR * D + NR + key] = part[key]; }
       }
       named_barrier_sync(1, 128);                                   // shift and part are the next segment's now
       ++nseg;
@@ -638,8 +656,17 @@ int launch(const AttnCall& c, const CUtensorMap& mk, const CUtensorMap& mv, cons
     set.done(dev);
   }
   r = launch_after(true, 1, dim3(ctas), dim3(kThreads), F::kSmem, c.stream, paged_few_kernel<D, NR>, mk, mv, p);
-  if (r != KVQ_OK) return r;
+  if (r != KVQ_OK || p.whole) return r;
   return launch_after(true, 1, dim3(ctas, (unsigned)(c.group * c.m_tokens)), dim3(D), 0, c.stream, paged_few_merge_kernel<D, NR>, p, ctas);
+}
+
+// A CTA for each unit and no merge, where there are no more units than SMs and their sequences are short (by the width of the table's rows, all that the host
+// knows of them).  Whole against cut, us from a graph: 2 units of 64 channels of 4 tiles 6.9 / 8.3, of 6 8.1 / 8.9, of 8 9.6 / 8.3; 128 units of 6 tiles
+// 10.1 / 14.6 (128 channels), of 12 14.3 / 18.3; 256 units of one tile 11.1 / 10.1.
+constexpr int kWholeTiles = 6, kWholeTilesMany = 12;
+bool take_whole(const AttnCall& c, int sms) {
+  const int64_t units = (int64_t)c.seqs.batch * c.pool.kv_heads, tokens = (int64_t)c.seqs.width * c.pool.page;
+  return units <= sms && tokens <= (2 * units > sms ? kWholeTilesMany : kWholeTiles) * kTileKeys;
 }
 
 size_t header_bytes(int ctas) { return ((size_t)ctas * 2 * sizeof(int4) + 255) / 256 * 256; }
@@ -671,6 +698,8 @@ int launch_attn_few(const AttnCall& c) {
   p.headers = static_cast<int4*>(c.workspace);
   p.slots = static_cast<uint8_t*>(c.workspace) + header_bytes(sms);
   p.wait_budget = wait_budget();
+  p.whole = take_whole(c, sms);
+  if (p.whole) { p.headers = nullptr; sms = c.seqs.batch * c.pool.kv_heads; }
   const int nr = rows_of(c.group, c.m_tokens);
   if (c.head_dim == 64) {
     if (nr == 8) return launch<64, 8>(c, mk, mv, p, sms);
