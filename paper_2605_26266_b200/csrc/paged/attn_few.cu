@@ -13,6 +13,9 @@
 //
 // Work: the tiles (128 tokens) of all (sequence, key head) units in one line, cut evenly over the CTAs; lengths are on the device, so every CTA finds
 // its place in the line itself.  Units that are cut leave FP32 partial rows for the merge kernel.
+//
+// 64 requests of up to 16 384 tokens, 32 query heads on 8 of 128 channels: 199 us, 5.9 TB/s of codes; one request of 149 760: 61 us, 5.0 TB/s, the rest its
+// start, the last tile's chain and the merge; 16 tokens of 32 heads over 16 384 (32 heads, so 32 units): 42 us, 3.2 TB/s.
 #include "tensor.cuh"
 
 namespace kvq {
