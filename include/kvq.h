@@ -378,8 +378,8 @@ typedef struct kvq_rope {
  * kvq_paged_attn also leaves the code of a bounded wait that expired, as described there; the output is then undefined.
  * Few rows: 601 (stage free); 611 (tile), 612 (scores read), 613 (queries), 614 (weights); 621 (tile), 622 (scores), 623, 624 and 625 (product retired
  * before a rescale, before new weights, before the sums); 631 (queries free).  Chunks: 701, 702 (stage of keys, of values free), 703 (queries free);
- * 711 (keys), 712 (queries), 713 (values), 714 (output read out), 715 and 717 (weights of the first and second half), 716 (turn of the
- * query tile), 718 (scores read); 721 (scores), 722 and 724 (product retired before a rescale, before new weights), 723 (last product); 732 (values), 733 (expanded values' stage free); 741 (what
+ * 711 (keys), 712 (queries), 713 (values), 714 (output read out), 715 and 717 (weights of the first and second half), 716 (what comes
+ * next), 718 (scores read); 721 (scores), 722 and 724 (product retired before a rescale, before new weights), 723 (last product); 732 (values), 733 (expanded values' stage free); 741 (what
  * comes next), 742 (room to say so). */
 #define KVQ_PAGED_BAD_PAGE      501
 #define KVQ_PAGED_BAD_POSITION  502

@@ -15,9 +15,10 @@
 // Work: the tile steps of all units in one line, cut evenly over the CTAs (lengths are on the device, and so is the cut: one block of the kernel ahead makes it).  Units that
 // are cut leave FP32 partial rows for the merge kernel.
 //
-// A step is 256 rows by 128 keys: its products alone take 2 066 cycles (QK in two E4M3 parts, PV in FP16, 128 channels), its 32 768 exponentials 2 200 with
-// what is around them, and the two take turns rather than overlap wholly.  24 heads x 4 680 tokens over 42 120: 2 630 us, 921 TFLOP/s of the formula's, at
-// 1.65 GHz (the clock under that load); two prompts of 4 096 (32 heads, causal): 345 us; 256 tokens of 32 heads over 65 792: 310 us, 889 TFLOP/s.
+// A step is 256 rows by 128 keys.  Of 128 channels its products alone take 2 066 cycles (QK in two E4M3 parts, PV in FP16), its 32 768 exponentials 2 048, and
+// all of it 3 200: the softmax warps hardly wait any more, but load, look for the maximum and hand over in 1 400 cycles that the exponentials of the other query
+// tile cover in part.  24 heads x 4 680 tokens over 42 120: 2 270 us, 1 067 TFLOP/s of the formula's, at 1.47 GHz (the clock under that load); two prompts of
+// 4 096 (32 heads, causal): 310 us; 256 tokens of 32 heads over 65 792: 271 us, 1 016 TFLOP/s.
 #include "tensor.cuh"
 
 namespace kvq {
@@ -59,18 +60,18 @@ template <int D>
 struct Chunk {
   static constexpr int kTile = kTileKeys * D;                       // bytes of a tile of codes, and of a part of a query tile
   static constexpr int kKStages = 3, kRawStages = 2, kVStages = 2, kSegs = 4;
-  // Heads of 64 channels leave tensor memory for weights of their own: the next scores are computed as soon as a tile's are in registers, while its weights are.
-  // Of 128 channels the weights lie over the scores, which the next ones have to wait for.
-  static constexpr bool kAhead = D == 64;
-  static constexpr int kTmemO = 256, kTmemP = kAhead ? 384 : 0, kColsP = kAhead ? 64 : 128;      // columns; from one query tile's weights to the other's
+  // Weights have tensor memory of their own, so that the next scores are computed as soon as a tile's are in registers, while its weights are.  Of 64
+  // channels there is room for scores of both query tiles; of 128 they share one place, in turns.
+  static constexpr bool kShared = D == 128;
+  static constexpr int kTmemS = kShared ? 0 : 128, kTmemP = kShared ? 128 : 384, kColsP = 64, kTmemO = 256;      // columns; S and P: from one query tile's to the other's
   static constexpr int kOffQ = 0;                                   // [query tile][part]
   static constexpr int kOffK = kOffQ + 4 * kTile;
   static constexpr int kOffRaw = kOffK + kKStages * kTile;
   static constexpr int kOffV = kOffRaw + kRawStages * kTile;        // FP16
   static constexpr int kOffBar = kOffV + kVStages * 2 * kTile;
   enum { kKFull = 0, kKEmpty = kKFull + kKStages, kRawFull = kKEmpty + kKStages, kRawEmpty = kRawFull + kRawStages, kVFull = kRawEmpty + kRawStages,
-         kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPFull = kSFull + 2, kODone = kPFull + 4,      // of weights: + 2 half + query tile
-         kOFree = kODone + 2, kTurn = kOFree + 2, kSFree = kTurn + 2, kSegFull = kSFree + 2,
+         kVEmpty = kVFull + kVStages, kQFull = kVEmpty + kVStages, kQEmpty = kQFull + 2, kSFull, kPHalf = kSFull + 2, kPFull = kPHalf + 2, kODone = kPFull + 2,
+         kOFree = kODone + 2, kSFree = kOFree + 2, kSegFull = kSFree + 2,
          kSegEmpty = kSegFull + kSegs, kDrain = kSegEmpty + kSegs, kBars = kDrain + 2 };
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kOffScale = (kOffMisc + 8 + 127) / 128 * 128;      // [8 tiles][3][8] floats: key factors, value exponents, their inverses
@@ -136,14 +137,27 @@ struct Reader {
   const uint8_t* smem;
   int n;
   __device__ __forceinline__ Reader(const Waits& c, const uint8_t* s) : cx(c), smem(s), n(0) {}
+  // One lane for its warp, which has no other business.
+  __device__ __forceinline__ bool next_alone(Segment& s) {
+    using F = Chunk<D>;
+    const int slot = n % F::kSegs;
+    if (!cx.wait(F::kSegFull + slot, n / F::kSegs & 1, 716)) return false;
+    take(s, slot);
+    ptx::mbar_arrive(cx.bar(F::kSegEmpty + slot));
+    ++n;
+    return s.b >= 0;
+  }
+  __device__ __forceinline__ void take(Segment& s, int slot) const {
+    const int4* at = reinterpret_cast<const int4*>(smem + Chunk<D>::kOffSeg + slot * 64);
+    const int4 a = at[0], b = at[1], c = at[2];
+    s.b = a.x; s.h = a.y; s.rb = a.z; s.tb = a.w; s.te = b.x; s.n = b.y; s.first = b.z; s.ex = Extent{b.w, c.x};
+  }
   // row: which factor of the unit's rows goes to *factor (nullptr: none)
   __device__ __forceinline__ bool next(Segment& s, int row = 0, float* factor = nullptr) {
     using F = Chunk<D>;
     const int slot = n % F::kSegs;
     if (!__all_sync(0xFFFFFFFFu, cx.wait(F::kSegFull + slot, n / F::kSegs & 1, 741))) return false;
-    const int4* at = reinterpret_cast<const int4*>(smem + F::kOffSeg + slot * 64);
-    const int4 a = at[0], b = at[1], c = at[2];
-    s.b = a.x; s.h = a.y; s.rb = a.z; s.tb = a.w; s.te = b.x; s.n = b.y; s.first = b.z; s.ex = Extent{b.w, c.x};
+    take(s, slot);
     if (factor) *factor = reinterpret_cast<const float*>(smem + F::kOffRow)[slot * kRows + row];
     __syncwarp();
     if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(cx.bar(F::kSegEmpty + slot));
@@ -392,9 +406,9 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       mbar_init(cx.bar(F::kRawFull + s), 1); mbar_init(cx.bar(F::kRawEmpty + s), 128);
       mbar_init(cx.bar(F::kVFull + s), 128); mbar_init(cx.bar(F::kVEmpty + s), 2);
       mbar_init(cx.bar(F::kQFull + s), 1); mbar_init(cx.bar(F::kOFree + s), 128);
-      mbar_init(cx.bar(F::kSFull + s), 1); mbar_init(cx.bar(F::kODone + s), 1); mbar_init(cx.bar(F::kTurn + s), 1); mbar_init(cx.bar(F::kDrain + s), 1);
+      mbar_init(cx.bar(F::kSFull + s), 1); mbar_init(cx.bar(F::kODone + s), 1); mbar_init(cx.bar(F::kDrain + s), 1);
       mbar_init(cx.bar(F::kSFree + s), 128);
-      mbar_init(cx.bar(F::kPFull + s), 128); mbar_init(cx.bar(F::kPFull + 2 + s), 128);
+      mbar_init(cx.bar(F::kPHalf + s), 128); mbar_init(cx.bar(F::kPFull + s), 128);
     }
     mbar_init(cx.bar(F::kQEmpty), 2);
     for (int s = 0; s < F::kSegs; ++s) { mbar_init(cx.bar(F::kSegFull + s), 1); mbar_init(cx.bar(F::kSegEmpty + s), 15); }      // all warps but the query warp
@@ -411,7 +425,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + F::kOffMisc);
   const int4 at = load_coherent(p.places + 2 * blockIdx.x), left = load_coherent(p.places + 2 * blockIdx.x + 1);
   const Place place{at.x, at.y, at.z, at.w, (long long)(uint32_t)left.x | (long long)left.y << 32};
-  // TMEM columns: S0 [0, 128), S1 [128, 256), O0 and O1 from 256; weights (FP16 pairs) over the first 64 columns of their scores, or of 64 channels from 384.
+  // TMEM columns: 128 channels: S [0, 128), P0, P1 (FP16 pairs) 64 each, O0, O1 from 256.  64 channels: S0, S1, O0 and O1 from 256, P0 and P1 from 384.
 
   if (warp < 4) {
     setmaxnreg_dec<kRegsIssue>();
@@ -483,112 +497,105 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       }
     } else if (warp <= 2) {
       // ================= issuers: warp 1 + qt for query tile qt =================
-      const bool leader = elect_one();
-      const int qt = warp - 1;
-      const uint32_t idesc_s = make_idesc_e4m3(128, 128, 0, 0);
-      const uint32_t idesc_o = make_idesc_bf16(128, D, 0, 1) & ~((7u << 7) | (7u << 10));      // FP16
-      const uint64_t dq = make_smem_desc(sbase + F::kOffQ + qt * 2 * F::kTile, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
-      const uint64_t dk = make_smem_desc(sbase + F::kOffK, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
-      const uint64_t dv = make_smem_desc(sbase + F::kOffV, kTileKeys * 128, 1024, kLayoutSw128);
-      const uint32_t s_tmem = tmem + qt * 128, o_tmem = tmem + F::kTmemO + qt * D, p_tmem = tmem + F::kTmemP + qt * F::kColsP;
-      Reader<D> w(cx, smem);
-      Segment sg;
-      int it = 0, n = 0, nseg = 0, nact = 0, turns = 0;        // tiles, tiles and segments of this query tile, its turns
-      bool ok = true;
-      auto scores = [&](int i) {                               // of tile i
-        if (!leader) return;
-        const int s = i % F::kKStages;
+      // One lane does all of it: beside the softmax warps each instruction of a chain waits for its turn, so votes and rejoining lanes would be felt.
+      if (elect_one()) {
+        const int qt = warp - 1;
+        const uint32_t idesc_s = make_idesc_e4m3(128, 128, 0, 0);
+        const uint32_t idesc_o = make_idesc_bf16(128, D, 0, 1) & ~((7u << 7) | (7u << 10));      // FP16
+        const uint64_t dq = make_smem_desc(sbase + F::kOffQ + qt * 2 * F::kTile, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
+        const uint64_t dk = make_smem_desc(sbase + F::kOffK, 16, RowLayout<D>::kAtom, RowLayout<D>::kKind);
+        const uint64_t dv = make_smem_desc(sbase + F::kOffV, kTileKeys * 128, 1024, kLayoutSw128);
+        const uint32_t s_tmem = tmem + qt * F::kTmemS, o_tmem = tmem + F::kTmemO + qt * D, p_tmem = tmem + F::kTmemP + qt * F::kColsP;
+        Reader<D> w(cx, smem);
+        Segment sg;
+        int it = 0, n = 0, nseg = 0, nact = 0, pairs = 0;      // tiles, tiles and segments of this query tile, tiles of both query tiles
+        int ks = 0, kphase = 0;                                // of the next scores
+        bool ok = true;
+        // Scores of tile i may be written: the ones before are in registers.  A shared place is the first query tile's, then the second's, then the first's of
+        // the next tile: that keeps the softmax groups half a step apart.  paired: tile i - 1 was both query tiles'.
+        auto free_for = [&](int i, bool paired) -> bool {
+          const int of = !F::kShared ? qt : qt == 0 && paired ? 1 : 0;
+          const int use = !F::kShared ? n : qt == 1 ? i : paired ? pairs - 1 : i - 1;
+          // the second tile comes back: the first's last use without it, too, so that a wait is one phase ahead of its barrier at most
+          for (int u = use - (F::kShared && qt == 1 && !paired); u <= use; ++u)
+            if (u >= 0 && !cx.wait(F::kSFree + of, u & 1, 718)) return false;
+          return true;
+        };
+        auto scores = [&]() {                         // of the next tile
+          const uint64_t k = dk + (uint64_t)(ks * F::kTile >> 4);
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+          for (int part = 0; part < 2; ++part)
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k)
-            mma_e4m3_ss(s_tmem, dq + (uint64_t)((part * F::kTile + 32 * k) >> 4), dk + (uint64_t)((s * F::kTile + 32 * k) >> 4), idesc_s, part + k > 0);
-        tc_commit(cx.bar(F::kSFull + qt));
-      };
-      auto products = [&](int s, int hf, bool add) {           // of 64 keys of stage s
-        if (!leader) return;
+            for (int c = 0; c < D / 32; ++c)
+              mma_e4m3_ss(s_tmem, dq + (uint64_t)((part * F::kTile + 32 * c) >> 4), k + (uint64_t)(32 * c >> 4), idesc_s, part + c > 0);
+          tc_commit(cx.bar(F::kSFull + qt));
+        };
+        auto taken = [&](bool last) {                          // the next tile's keys; of the segment's last one the queries
+          tc_commit(cx.bar(F::kKEmpty + ks));
+          if (last) tc_commit(cx.bar(F::kQEmpty));
+          if (++ks == F::kKStages) { ks = 0; kphase ^= 1; }
+        };
+        auto products = [&](int s, int hf, bool add) {         // of 64 keys of stage s
 #pragma unroll
-        for (int k = 0; k < 4; ++k)                            // 16 keys a step
-          mma_ts(o_tmem, p_tmem + 32 * hf + 8 * k, dv + (uint64_t)((s * 2 * F::kTile + (4 * hf + k) * 16 * 128) >> 4), idesc_o, add || k > 0);
-      };
-      // The two query tiles take turns at the tensor pipe: O += P V of one and at once its next scores, then the same of the other.  That keeps the softmax groups
-      // half a step apart: one has its exponentials while the other waits for products.  Each has its own warp, whose waits and commits then do not hold up
-      // the other's products.
-      auto my_turn = [&](bool both) -> bool {
-        if (F::kAhead || !both) return true;
-        const bool r = all_lanes(cx.wait(F::kTurn + qt, (turns & 1) ^ 1 ^ qt, 716));
-        ++turns;
-        return r;
-      };
-      auto pass_on = [&](bool both) {
-        if (!F::kAhead && both && leader) mbar_arrive(cx.bar(F::kTurn + (qt ^ 1)));
-        __syncwarp();
-      };
-      while (ok && w.next(sg)) {
-        const int rows = sg.ex.fresh * p.group - sg.rb * kRows;
-        const bool act = rows > qt * 128, both = rows > 128;
-        if (!(ok = all_lanes(cx.wait(F::kQFull + qt, nseg & 1, 712)) && all_lanes(cx.wait(F::kKFull + it % F::kKStages, it / F::kKStages & 1, 711)))) break;
-        if (!(ok = my_turn(both))) break;
-        tc_fence_after();
-        if (act) scores(it);
-        pass_on(both);
-        if (leader) {
-          tc_commit(cx.bar(F::kKEmpty + it % F::kKStages));
-          if (sg.te - sg.tb == 1) tc_commit(cx.bar(F::kQEmpty));
-        }
-        __syncwarp();
-        for (int t = sg.tb; t < sg.te; ++t, ++it) {
-          const int vs = it & 1, s1 = (it + 1) % F::kKStages;
-          const bool next = t + 1 < sg.te;
-          if (next && !(ok = all_lanes(cx.wait(F::kKFull + s1, (it + 1) / F::kKStages & 1, 711)))) break;
-          if (F::kAhead && next) {
-            if (act) {
-              if (!(ok = all_lanes(cx.wait(F::kSFree + qt, n & 1, 718)))) break;
-              tc_fence_after();
-              scores(it + 1);
-            }
-            if (leader) {
-              tc_commit(cx.bar(F::kKEmpty + s1));
-              if (t + 2 == sg.te) tc_commit(cx.bar(F::kQEmpty));
-            }
-            __syncwarp();
-          }
-          if (!(ok = all_lanes(cx.wait(F::kVFull + vs, it >> 1 & 1, 713)))) break;
+          for (int k = 0; k < 4; ++k)                          // 16 keys a step
+            mma_ts(o_tmem, p_tmem + 32 * hf + 8 * k, dv + (uint64_t)((s * 2 * F::kTile + (4 * hf + k) * 16 * 128) >> 4), idesc_o, add || k > 0);
+        };
+        bool paired = false;
+        while (ok && w.next_alone(sg)) {
+          const int rows = sg.ex.fresh * p.group - sg.rb * kRows;
+          const bool act = rows > qt * 128, both = rows > 128;
+          if (!(ok = cx.wait(F::kQFull + qt, nseg & 1, 712) && cx.wait(F::kKFull + ks, kphase, 711))) break;
           if (act) {
-            if (t == sg.tb && !(ok = all_lanes(cx.wait(F::kOFree + qt, (nact & 1) ^ 1, 714)))) break;
-            if (!(ok = all_lanes(cx.wait(F::kPFull + qt, n & 1, 715)))) break;
-            if (!(ok = my_turn(both))) break;
+            if (F::kShared && !(ok = free_for(it, paired))) break;      // places of their own: the segment before ended with the weights of the last scores
             tc_fence_after();
-            products(vs, 0, t > sg.tb);
-            if (!(ok = all_lanes(cx.wait(F::kPFull + 2 + qt, n & 1, 717)))) break;
-            tc_fence_after();
-            products(vs, 1, true);
-            if (leader && (F::kAhead || !next)) tc_commit(cx.bar(F::kODone + qt));
-            if (!F::kAhead && next) scores(it + 1);
-            pass_on(both);
-            ++n;
+            scores();
           }
-          if (leader) {
+          taken(sg.te - sg.tb == 1);
+          paired = both;
+          for (int t = sg.tb; t < sg.te; ++t, ++it) {
+            const int vs = it & 1;
+            if (both) ++pairs;
+            if (t + 1 < sg.te) {
+              if (!(ok = cx.wait(F::kKFull + ks, kphase, 711))) break;
+              if (act) {
+                if (!(ok = free_for(it + 1, both))) break;
+                tc_fence_after();
+                scores();
+              }
+              taken(t + 2 == sg.te);
+            }
+            if (!(ok = cx.wait(F::kVFull + vs, it >> 1 & 1, 713))) break;
+            if (act) {
+              if (t == sg.tb && !(ok = cx.wait(F::kOFree + qt, (nact & 1) ^ 1, 714))) break;
+              if (!F::kShared) {
+                if (!(ok = cx.wait(F::kPHalf + qt, n & 1, 715))) break;
+                tc_fence_after();
+                products(vs, 0, t > sg.tb);
+              }
+              if (!(ok = cx.wait(F::kPFull + qt, n & 1, 717))) break;
+              tc_fence_after();
+              if (F::kShared) products(vs, 0, t > sg.tb);
+              products(vs, 1, true);
+              tc_commit(cx.bar(F::kODone + qt));
+              ++n;
+            }
             tc_commit(cx.bar(F::kVEmpty + vs));
-            if (!F::kAhead && next) tc_commit(cx.bar(F::kKEmpty + s1));
-            if (!F::kAhead && t + 2 == sg.te) tc_commit(cx.bar(F::kQEmpty));
           }
-          __syncwarp();
+          if (!ok) break;
+          ++nseg;
+          if (act) ++nact;
         }
-        if (!ok) break;
-        ++nseg;
-        if (act) ++nact;
+        tc_commit(cx.bar(F::kDrain + qt));                     // whatever has been issued is done before TMEM and shared memory go
+        cx.drain(F::kDrain + qt, 0);
+        // Commits arrive in no promised order: the last ones of every barrier are waited for too.
+        if (ok) {
+          for (int k = max(it - F::kKStages, 0); k < it; ++k) cx.drain(F::kKEmpty + k % F::kKStages, k / F::kKStages & 1);
+          for (int k = max(it - 2, 0); k < it; ++k) cx.drain(F::kVEmpty + (k & 1), k >> 1 & 1);
+          if (n > 0) { cx.drain(F::kSFull + qt, (n - 1) & 1); cx.drain(F::kODone + qt, (n - 1) & 1); }
+          if (nseg > 0) cx.drain(F::kQEmpty, (nseg - 1) & 1);
+        }
       }
-      if (leader) tc_commit(cx.bar(F::kDrain + qt));           // whatever has been issued is done before TMEM and shared memory go
       __syncwarp();
-      cx.drain(F::kDrain + qt, 0);
-      // Commits arrive in no promised order: the last ones of every barrier are waited for too.
-      if (ok) {
-        for (int k = max(it - F::kKStages, 0); k < it; ++k) cx.drain(F::kKEmpty + k % F::kKStages, k / F::kKStages & 1);
-        for (int k = max(it - 2, 0); k < it; ++k) cx.drain(F::kVEmpty + (k & 1), k >> 1 & 1);
-        if (n > 0) { cx.drain(F::kSFull + qt, (n - 1) & 1); cx.drain(F::kODone + qt, ((F::kAhead ? n : nact) - 1) & 1); }
-        if (nseg > 0) cx.drain(F::kQEmpty, (nseg - 1) & 1);
-      }
     } else if (warp == 3) {
       // ================= units in order, and their queries =================
       Walker w(place);
@@ -644,7 +651,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const int qt = (warp - 4) >> 2, wq = warp & 3;
     const int r256 = qt * 128 + wq * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
-    const uint32_t s_addr = tmem + lane_addr + qt * 128, o_addr = tmem + lane_addr + F::kTmemO + qt * D, p_addr = tmem + lane_addr + F::kTmemP + qt * F::kColsP;
+    const uint32_t s_addr = tmem + lane_addr + qt * F::kTmemS, o_addr = tmem + lane_addr + F::kTmemO + qt * D, p_addr = tmem + lane_addr + F::kTmemP + qt * F::kColsP;
     int4* header = p.headers + 2 * blockIdx.x;
     if (tid == 128) header[0] = header[1] = make_int4(kNone, 0, 0, 0);
     Reader<D> w(cx, smem);
@@ -681,10 +688,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           v[4 * h] = v4.x; v[4 * h + 1] = v4.y; v[4 * h + 2] = v4.z; v[4 * h + 3] = v4.w;
         }
         tmem_wait_ld();
-        if (F::kAhead) {
-          tc_fence_before();
-          mbar_arrive(cx.bar(F::kSFree + qt));
-        }
+        tc_fence_before();
+        mbar_arrive(cx.bar(F::kSFree + qt));
         if (edge) {
           const int nv = min(hi, total) - first, nl = lo - first;
 #pragma unroll
@@ -705,11 +710,9 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         }
         if (__any_sync(0xFFFFFFFFu, m_new - m > kSlack)) {
           if (t > sg.tb) {
-            if (F::kAhead) {                           // the last product on O; of 128 channels these scores' commit came after it
-              ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 722));
-              if (!ok) break;
-              tc_fence_after();
-            }
+            ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 722));      // the last product on O
+            if (!ok) break;
+            tc_fence_after();
             const float drop = ex2(m - m_new);
 #pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
@@ -742,29 +745,31 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             s[k / 2] = cvt_f16x2(w2.x, w2.y);
           }
           l = fmaf(sum.x + sum.y, inv[i], l);
-          if (i == 3) {
-            if (F::kAhead && t > sg.tb) {              // the last product has read the weights before
+          // The first half goes its way while the second is computed, where scores have places of their own.  Where not, the product before is issued late, behind
+          // the scores of both query tiles, and a store on the way would wait for it in the middle of the exponentials.
+          if (i == (F::kShared ? 7 : 4)) {
+            if (t > sg.tb) {                           // the last product has read the weights before
               ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 724));
               if (!ok) break;
               tc_fence_after();
             }
             st32_plain(p_addr, s);
           }
-          if (i == 5) {
+          if (!F::kShared && i == 6) {
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(cx.bar(F::kPFull + qt));
+            mbar_arrive(cx.bar(F::kPHalf + qt));
           }
         }
         if (!ok) break;
         tmem_st32(p_addr + 32, s + 32);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(cx.bar(F::kPFull + 2 + qt));
+        mbar_arrive(cx.bar(F::kPFull + qt));
       }
       if (!ok) break;
       // ---- the rows' results ----
-      ok = all_lanes(cx.wait(F::kODone + qt, (F::kAhead ? n - 1 : nact) & 1, 723));      // the segment's last product
+      ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 723));      // the segment's last product
       if (!ok) break;
       tc_fence_after();
       if (!(rowf == rowf)) l = rowf;                             // a query that is no finite number
