@@ -14,8 +14,8 @@
 // Work: the tiles (128 tokens) of all (sequence, key head) units in one line, cut evenly over the CTAs; lengths are on the device, so every CTA finds
 // its place in the line itself.  Units that are cut leave FP32 partial rows for the merge kernel.
 //
-// 64 requests of up to 16 384 tokens, 32 query heads on 8 of 128 channels: 199 us, 5.9 TB/s of codes; one request of 149 760: 61 us, 5.0 TB/s, the rest its
-// start, the last tile's chain and the merge; 16 tokens of 32 heads over 16 384 (32 heads, so 32 units): 42 us, 3.2 TB/s.
+// 64 requests of up to 16 384 tokens, 32 query heads on 8 of 128 channels: 199 to 209 us, 5.7 to 5.9 TB/s of codes; one request of 149 760: 61 us, 5.0 TB/s, the
+// rest its start, the last tile's chain and the merge; 16 tokens of 32 heads over 16 384: 38 us, 3.6 TB/s, of which 25 are the bytes'.
 #include "tensor.cuh"
 
 namespace kvq {
@@ -42,7 +42,7 @@ struct FewParams {
   uint32_t wait_budget;
 };
 
-constexpr int kThreads = 256;      // producer, issuer, two warps for rows without keys, four softmax warps
+constexpr int kThreads = 384;      // producer, issuer, two warps for queries and rows without keys, two groups of four softmax warps
 constexpr float kBase = 5.f, kSlack = 3.f;
 enum { kNone = 0, kStart = 1, kMiddle = 2, kEnd = 3 };
 
@@ -62,12 +62,12 @@ struct Few {
          kDrain = kPDone + 2, kBars };
   static constexpr int kOffMisc = kOffBar + kBars * 8;              // tmem base, abort
   static constexpr int kOffScale = (kOffMisc + 8 + 15) / 16 * 16;   // [stages][2][8] scale bytes of a tile's pages
-  static constexpr int kOffRow = kOffScale + kStages * 16;          // floats: row factors of two segments, 5 - m, f, partial maxima and sums [4][NR]
-  static constexpr int kOffAcc = kOffRow + (4 + 4) * NR * 4;        // whether the product of a buffer adds to O^T
+  static constexpr int kOffRow = kOffScale + kStages * 16;          // floats: row factors of two segments; of the two groups: 5 - m, f, partial maxima and sums [4][NR]
+  static constexpr int kOffAcc = kOffRow + (2 + 2 * 6) * NR * 4;    // whether the product of a buffer adds to O^T
   static constexpr int kOffWalk = (kOffAcc + 8 + 15) / 16 * 16;
   static constexpr int kSmem = kOffWalk + 48 + 1024;
   static constexpr int kTmemS = 0, kTmemO = 2 * kN;
-  static constexpr int kTmemCols = 2 * kN + kNP <= 128 ? 128 : 256;
+  static constexpr int kTmemCols = 2 * kN + 2 * kNP <= 128 ? 128 : 2 * kN + 2 * kNP <= 256 ? 256 : 512;
   static constexpr int kSlotBytes = NR * (D + 2) * 4;
 };
 
@@ -307,8 +307,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       if (!(ok = all(cx.wait(F::kQFull, nseg & 1, 613)))) break;
       tc_fence_after();
       if (!(ok = scores(it, sg.te - sg.tb == 1))) break;
+      if (sg.te - sg.tb > 1 && !(ok = scores(it + 1, sg.te - sg.tb == 2))) break;
       for (int t = sg.tb; t < sg.te; ++t, ++it) {
-        if (t + 1 < sg.te && !(ok = scores(it + 1, t + 2 == sg.te))) break;
+        if (t + 2 < sg.te && !(ok = scores(it + 2, t + 3 == sg.te))) break;      // as soon as those of tile t are in registers
         const int s = it % F::kStages, buf = it & 1;
         if (!(ok = all(cx.wait(F::kPFull + buf, it >> 1 & 1, 614)))) break;
         tc_fence_after();
@@ -316,7 +317,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           const uint32_t add = (uint32_t)accumulate[buf];
 #pragma unroll
           for (int k = 0; k < 4; ++k)                      // 32 keys a step
-            mma_e4m3_ss(tmem + F::kTmemO, dv + (uint64_t)((s * 2 * F::kTile + 32 * k * D) >> 4),
+            mma_e4m3_ss(tmem + F::kTmemO + buf * F::kNP, dv + (uint64_t)((s * 2 * F::kTile + 32 * k * D) >> 4),
                         dp + (uint64_t)((buf * F::kPBytes + k * 512) >> 4), idesc_o, k > 0 ? 1u : add);
           tc_commit(cx.bar(F::kEmpty + s));
           tc_commit(cx.bar(F::kPDone + buf));
@@ -405,57 +406,72 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
     }
   } else {
-    // ================= softmax: a key of the tile a thread =================
-    const int key = tid - 128, wq = warp & 3;
+    // ================= softmax: a key of the tile a thread, every other tile a group =================
+    // A tile's way through a group is a chain of some 1 600 cycles with 16 rows, as long as its bytes take; so two groups have a tile each, their own maxima, sums
+    // and O^T, and are joined at the segment's end.  16 tokens of 32 heads over 16 384: one group 41.3 us, two 37.7; 64 requests of a token 211 and 205.
+    const int grp = (warp - 4) >> 2, key = (tid - 128) & 127, wq = warp & 3;
     const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
     const float* rowfs = reinterpret_cast<const float*>(smem + F::kOffRow);      // factors of the rows' scores, of two segments
-    float* shift = reinterpret_cast<float*>(smem + F::kOffRow) + 2 * NR;         // 5 - m
-    float* drop = shift + NR;                                       // 2^(old m - new m)
-    float* part = drop + NR;                                        // [4][NR]
+    float* shifts = reinterpret_cast<float*>(smem + F::kOffRow) + 2 * NR;
+    float* shift = shifts + grp * NR;                               // 5 - m
+    float* drop = shifts + (2 + grp) * NR;                          // 2^(old m - new m)
+    float* part = shifts + (4 + 4 * grp) * NR;                      // [4][NR]
     volatile int* accumulate = reinterpret_cast<volatile int*>(smem + F::kOffAcc);
+    const uint32_t s_addr = tmem + lane_addr + F::kTmemS + grp * F::kN, o_addr = tmem + lane_addr + F::kTmemO + grp * F::kNP;
+    const uint32_t bar_id = 1 + grp;
     const int rows = p.group * p.m_tokens;
     int4* header = p.headers + 2 * blockIdx.x;
-    if (key == 0 && p.headers) header[0] = header[1] = make_int4(kNone, 0, 0, 0);
+    if (tid == 128 && p.headers) header[0] = header[1] = make_int4(kNone, 0, 0, 0);
     Walker w(place);
     Segment sg;
-    int it = 0, nseg = 0;
+    int it0 = 0, nseg = 0;                                          // the segment's first tile; a tile is of the group of its lowest bit
     bool ok = true;
     while (ok && w.next(sg, p)) {
-      const int total = sg.ex.before + sg.ex.fresh;
+      const int total = sg.ex.before + sg.ex.fresh, tiles = sg.te - sg.tb;
       const float* rowf = rowfs + (nseg & 1) * NR;
       if (key < NR) shift[key] = kBase + 1e30f;
-      named_barrier_sync(1, 128);
-      float l[NR], o[NR];
+      named_barrier_sync(bar_id, 128);
+      float l[NR];
 #pragma unroll
-      for (int r = 0; r < NR; ++r) l[r] = o[r] = 0.f;
+      for (int r = 0; r < NR; ++r) l[r] = 0.f;
       bool fresh = true;                                            // nothing of this segment is in TMEM's O^T
-      for (int t = sg.tb; t < sg.te; ++t, ++it) {
-        const int s = it % F::kStages, buf = it & 1;
+      for (int it = it0 + ((it0 ^ grp) & 1); it < it0 + tiles; it += 2) {
+        const int s = it % F::kStages, tile0 = (sg.first + sg.tb + it - it0) * kTileKeys;
         // A wait that gives up does not end a warp's turn at the barriers of the four: the vote below ends it for all.
         ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kFull + s, it / F::kStages & 1, 621));      // the scales
         const int pg = key >> p.pool.log2_page;
         const uint32_t kb = smem[F::kOffScale + s * 16 + pg], vb = smem[F::kOffScale + s * 16 + 8 + pg];
-        const int j = (sg.first + t) * kTileKeys + key;             // the key's place in the sequence
+        const int j = tile0 + key;                                  // the key's place in the sequence
         const bool there = kb != 255 && j < total;
         const float kf = pow2(scale_exponent(kb));
         const int ve = scale_exponent(vb);
-        ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kSFull + buf, it >> 1 & 1, 622));
+        ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kSFull + grp, it >> 1 & 1, 622));
         tc_fence_after();
         float x[NR];
         {
-          uint32_t raw[F::kN];
-          tmem_load<F::kN>(tmem + lane_addr + F::kTmemS + buf * F::kN, raw);
-          tmem_wait_ld();
-          tc_fence_before();
-          mbar_arrive(cx.bar(F::kSFree + buf));
+          constexpr int kRows = NR == 8 ? 8 : 16;                   // rows at a time
 #pragma unroll
-          for (int r = 0; r < NR; ++r) {
-            const float a = fmaf(__uint_as_float(raw[2 * NR + r]), 0x1p-8f, fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r])));
-            x[r] = fmaf(a, rowf[r] * kf, (float)ve);
+          for (int r0 = 0; r0 < NR; r0 += kRows) {
+            uint32_t raw[F::kN == 32 ? 32 : 48];
+            if constexpr (NR == 8) tmem_ld32(s_addr, raw);
+            else {
+#pragma unroll
+              for (int i = 0; i < 3; ++i) tmem_ld16(s_addr + i * NR + r0, raw + i * 16);
+            }
+            tmem_wait_ld();
+            if (r0 + kRows == NR) {
+              tc_fence_before();
+              mbar_arrive(cx.bar(F::kSFree + grp));
+            }
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+              const float a = fmaf(__uint_as_float(raw[2 * kRows + r]), 0x1p-8f, fmaf(__uint_as_float(raw[kRows + r]), 0x1p-4f, __uint_as_float(raw[r])));
+              x[r0 + r] = fmaf(a, rowf[r0 + r] * kf, (float)ve);
+            }
           }
         }
         // keys that a row does not see; whole tiles that all rows see need no test
-        const int tile0 = (sg.first + t) * kTileKeys, seen = p.causal ? sg.ex.before + 1 : total;      // what the first row sees
+        const int seen = p.causal ? sg.ex.before + 1 : total;       // what the first row sees
         if (tile0 + kTileKeys > seen || (p.window && tile0 <= sg.ex.before + sg.ex.fresh - 1 - p.window) || __any_sync(0xFFFFFFFFu, !there)) {
           int at = sg.ex.before, g = 0;                             // the row's place in the sequence, without a division each
           const int back = p.window ? p.window : 0x7FFFFFFF;
@@ -468,34 +484,38 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         bool over = false;
 #pragma unroll
         for (int r = 0; r < NR; ++r) over |= x[r] + shift[r] > kBase + kSlack;
-        if (barrier_or(1, 128, over || !ok)) {                      // a row's maximum has to be raised
-          if (barrier_or(1, 128, !ok)) { ok = false; break; }
+        if (barrier_or(bar_id, 128, over || !ok)) {                 // a row's maximum has to be raised
+          if (barrier_or(bar_id, 128, !ok)) { ok = false; break; }
 #pragma unroll
           for (int r = 0; r < NR; ++r) {
             const float m = warp_max(x[r]);
             if (lane == 0) part[wq * NR + r] = m;
           }
-          named_barrier_sync(1, 128);
+          named_barrier_sync(bar_id, 128);
           if (key < NR) {
             const float old = kBase - shift[key];
             const float m = fmaxf(fmaxf(fmaxf(part[key], part[NR + key]), fmaxf(part[2 * NR + key], part[3 * NR + key])), old);
             drop[key] = ex2(old - m);
             shift[key] = kBase - m;
           }
-          if (!fresh) ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + (buf ^ 1), (it - 1) >> 1 & 1, 623));
-          named_barrier_sync(1, 128);
+          if (!fresh) ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + grp, ((it >> 1) - 1) & 1, 623));
+          named_barrier_sync(bar_id, 128);
           if (!fresh) {
-            uint32_t raw[F::kNP];
             tc_fence_after();
-            tmem_load<F::kNP>(tmem + lane_addr + F::kTmemO, raw);
-            tmem_wait_ld();
-            tc_fence_before();
 #pragma unroll
-            for (int r = 0; r < NR; ++r) o[r] += fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r]));
+            for (int c = 0; c < F::kNP; c += 16) {
+              uint32_t raw[16];
+              tmem_ld16(o_addr + c, raw);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) raw[i] = __float_as_uint(__uint_as_float(raw[i]) * drop[(c + i) % NR]);
+              tmem_st16(o_addr + c, raw);
+            }
+            tmem_wait_st();
+            tc_fence_before();
           }
 #pragma unroll
-          for (int r = 0; r < NR; ++r) { o[r] *= drop[r]; l[r] *= drop[r]; }
-          fresh = true;
+          for (int r = 0; r < NR; ++r) l[r] *= drop[r];
         }
         const float inv_v = pow2(max(-ve, -126));
 #pragma unroll
@@ -503,7 +523,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           x[r] = ex2(x[r] + shift[r]);
           l[r] = fmaf(x[r], inv_v, l[r]);
         }
-        ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + buf, (it >> 1 & 1) ^ 1, 624));      // the product that read this buffer
+        ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + grp, (it >> 1 & 1) ^ 1, 624));      // the product that read this buffer
         uint32_t hi[NR / 4], lo[NR / 4];
 #pragma unroll
         for (int r = 0; r < NR; r += 2) {
@@ -513,7 +533,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           if (r & 2) { hi[r / 4] |= h << 16; lo[r / 4] |= rest << 16; }
           else { hi[r / 4] = h; lo[r / 4] = rest; }
         }
-        uint4* dst = reinterpret_cast<uint4*>(smem + F::kOffP + buf * F::kPBytes + key * 16);
+        uint4* dst = reinterpret_cast<uint4*>(smem + F::kOffP + grp * F::kPBytes + key * 16);
         if constexpr (NR == 8) {
           dst[0] = make_uint4(hi[0], hi[1], lo[0], lo[1]);
         } else {
@@ -523,43 +543,79 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             dst[(NR / 16 + i) * kTileKeys] = make_uint4(lo[4 * i], lo[4 * i + 1], lo[4 * i + 2], lo[4 * i + 3]);
           }
         }
-        if (key == 0) accumulate[buf] = fresh ? 0 : 1;
+        if (key == 0) accumulate[grp] = fresh ? 0 : 1;
         fresh = false;
         fence_proxy_async_smem();
         tc_fence_before();
-        mbar_arrive(cx.bar(F::kPFull + buf));
+        mbar_arrive(cx.bar(F::kPFull + grp));
       }
-      // ---- the rows' sums: l over the 128 keys of a thread each, O^T from TMEM, a channel a thread ----
-      ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + ((it - 1) & 1), (it - 1) >> 1 & 1, 625));
-      if (barrier_or(1, 128, !ok)) { ok = false; break; }
-      {
-        // over the buffers of the weights, whose last product is done
-        float* sums = reinterpret_cast<float*>(smem + F::kOffP);
+      // ---- the rows' sums: l over the 128 keys of a thread each, O^T from TMEM, a channel a thread; the second group's go to the first ----
+      it0 += tiles;
+      const int mine = it0 - 1 - ((it0 - 1 ^ grp) & 1);             // the group's last tile, if it is this segment's
+      const bool any = mine >= it0 - tiles, two = tiles > 1 || (it0 - 1 & 1);      // the second group has one
+      if (any) ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + grp, mine >> 1 & 1, 625));
+      if (barrier_or(3, 256, !ok)) { ok = false; break; }
+      // over the buffers of the weights, whose last products are done
+      float* sums = reinterpret_cast<float*>(smem + F::kOffP);
+      auto factor = [&](int r) { return ex2(fminf(shifts[r], shifts[NR + r]) - shift[r]); };      // to the maximum of both groups
+      if (two) {
+        if (grp == 1) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) sums[r * 128 + key] = l[r] * factor(r);
+        }
+        named_barrier_sync(3, 256);
+        if (grp == 0) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) l[r] = fmaf(l[r], factor(r), sums[r * 128 + key]);
+        }
+      }
+      if (grp == 0) {
         constexpr int kPer = 128 / NR;                              // threads of a row
 #pragma unroll
         for (int r = 0; r < NR; ++r) sums[r * 128 + key] = l[r];
         named_barrier_sync(1, 128);
-        const float4* mine = reinterpret_cast<const float4*>(sums + key / kPer * 128) + key % kPer;
+        const float4* from = reinterpret_cast<const float4*>(sums + key / kPer * 128) + key % kPer;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NR / 4; ++i) {
-          const float4 x = mine[i * kPer];
+          const float4 x = from[i * kPer];
           sum += (x.x + x.y) + (x.z + x.w);
         }
 #pragma unroll
         for (int i = kPer / 2; i; i >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
         if (key % kPer == 0) { part[key / kPer] = sum; drop[key / kPer] = sum == 0.f ? 0.f : 1.f / sum; }
-        named_barrier_sync(1, 128);
       }
-      tc_fence_after();
-      {
+      float o[NR];
+#pragma unroll
+      for (int r = 0; r < NR; ++r) o[r] = 0.f;
+      if (any) {
+        tc_fence_after();
         uint32_t raw[F::kNP];
-        tmem_load<F::kNP>(tmem + lane_addr + F::kTmemO, raw);
+        tmem_load<F::kNP>(o_addr, raw);
         tmem_wait_ld();
         tc_fence_before();
 #pragma unroll
-        for (int r = 0; r < NR; ++r) o[r] += fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r]));
+        for (int r = 0; r < NR; ++r) o[r] = fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r]));
       }
+      if (two) {
+        named_barrier_sync(3, 256);                                 // sums are read
+        if (grp == 1) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) sums[r * 128 + key] = o[r] * factor(r);
+        }
+        named_barrier_sync(3, 256);
+        if (grp == 0) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) o[r] = fmaf(o[r], factor(r), sums[r * 128 + key]);
+        }
+      }
+      if (grp == 1) {
+        named_barrier_sync(3, 256);                                 // buffers and maxima are the next segment's now
+        ++nseg;
+        continue;
+      }
+      named_barrier_sync(1, 128);                                   // sums of the rows; nobody needs the maxima apart any more
+      if (key < NR) shift[key] = fminf(shifts[key], shifts[NR + key]);
       const bool whole = sg.tb == 0 && sg.te == sg.n;
       const int slot = nseg == 0 ? 0 : 1;
       float* to = whole ? nullptr : reinterpret_cast<float*>(p.slots + (size_t)(2 * blockIdx.x + slot) * F::kSlotBytes);
@@ -587,7 +643,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           if (key < D && r < used) to[r * D + key] = o[r];
         if (key < used) { to[NR * D + key] = -shift[key]; to[NR * D + NR + key] = part[key]; }
       }
-      named_barrier_sync(1, 128);                                   // shift and part are the next segment's now
+      named_barrier_sync(3, 256);                                   // shift and part are the next segment's now
       ++nseg;
     }
     tc_fence_before();
