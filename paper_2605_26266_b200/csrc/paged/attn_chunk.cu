@@ -17,8 +17,9 @@
 //
 // A step is 256 rows by 128 keys.  Of 128 channels its products alone take 2 066 cycles (QK in two E4M3 parts, PV in FP16), its 32 768 exponentials 2 048, and
 // all of it 3 200: the softmax warps hardly wait any more, but load, look for the maximum and hand over in 1 400 cycles that the exponentials of the other query
-// tile cover in part.  24 heads x 4 680 tokens over 42 120: 2 270 us, 1 067 TFLOP/s of the formula's, at 1.47 GHz (the clock under that load); two prompts of
-// 4 096 (32 heads, causal): 310 us; 256 tokens of 32 heads over 65 792: 271 us, 1 016 TFLOP/s.
+// tile cover in part.  24 heads x 4 680 tokens over 42 120: 2 270 to 2 320 us, 1 040 to 1 070 TFLOP/s of the formula's, at 1.40 to 1.47 GHz (power holds the
+// clock there under that load); two prompts of 4 096 (32 heads, causal): 310 us; 256 tokens of 32 heads over 65 792: 275 us, 1 000 TFLOP/s.  Of 64 channels a
+// step has half of the products and as many exponentials, which bound it: 2 200 cycles.
 #include "tensor.cuh"
 
 namespace kvq {
@@ -52,16 +53,20 @@ struct ChunkParams {
 
 constexpr int kThreads = 512;      // producer, two issuers, queries; two softmax groups; expanding warps
 constexpr int kRows = 256;
-constexpr int kRegsIssue = 48, kRegsSoftmax = 192, kRegsExpand = 80;      // 128 (48 + 2 * 192 + 80) = 512 * 128
+constexpr int kRegsIssue = 48;
 constexpr float kBase = 4.f, kSlack = 8.f, kNoMax = -1e30f, kLeast = 1.17549435e-38f;
 enum { kNone = 0, kStart = 1, kMiddle = 2, kEnd = 3 };
 
 template <int D>
 struct Chunk {
+  // 128 (48 + 2 * 192 + 80) = 128 (48 + 2 * 200 + 64) = 512 * 128.  64 channels need fewer to expand values: 79.6 us against 80.6 (12 sequences with a window);
+  // 128 channels with 200: two prompts of 4 096 316 us against 310.
+  static constexpr int kRegsSoftmax = D == 64 ? 200 : 192, kRegsExpand = D == 64 ? 64 : 80;
   static constexpr int kTile = kTileKeys * D;                       // bytes of a tile of codes, and of a part of a query tile
   static constexpr int kKStages = 3, kRawStages = 2, kVStages = 2, kSegs = 4;
   // Weights have tensor memory of their own, so that the next scores are computed as soon as a tile's are in registers, while its weights are.  Of 64
-  // channels there is room for scores of both query tiles; of 128 they share one place, in turns.
+  // channels there is room for scores of both query tiles; of 128 they share one place, in turns (24 x 4 680 over 42 120: 2 390 us, of which the late store of
+  // weights saves another 120; weights over their scores, which the next scores then wait for, 2 605).
   static constexpr bool kShared = D == 128;
   static constexpr int kTmemS = kShared ? 0 : 128, kTmemP = kShared ? 128 : 384, kColsP = 64, kTmemO = 256;      // columns; S and P: from one query tile's to the other's
   static constexpr int kOffQ = 0;                                   // [query tile][part]
@@ -82,8 +87,8 @@ struct Chunk {
   static constexpr int kSlotBytes = kSlotStats + 2 * kRows * 4;
 };
 
-// The line of tile steps: a unit counts kUnitSteps for its start and end, which take about as long (outputs, first loads and scores: 8 000 to 10 000 cycles;
-// without them CTAs with the short first blocks of causal prompts took 1.3 times as long as the others), then one for each tile.
+// The line of tile steps: a unit counts kUnitSteps for its start and end, which take about as long (outputs, first loads and scores: 5 000 to 8 000 cycles;
+// without them CTAs with the short first blocks of causal prompts took 1.3 times as long as the others; two prompts of 4 096: 309 us with 2, 311 with 3, 314 with 4), then one for each tile.
 constexpr int kUnitSteps = 2;
 __device__ __forceinline__ int tile_at(long long steps, int tiles) { return (int)min((long long)tiles, max(steps - kUnitSteps, 0ll)); }
 
@@ -647,7 +652,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     }
   } else if (warp < 12) {
     // ================= softmax: a query row a thread =================
-    setmaxnreg_inc<kRegsSoftmax>();
+    setmaxnreg_inc<F::kRegsSoftmax>();
     const int qt = (warp - 4) >> 2, wq = warp & 3;
     const int r256 = qt * 128 + wq * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
@@ -746,7 +751,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           }
           l = fmaf(sum.x + sum.y, inv[i], l);
           // The first half goes its way while the second is computed, where scores have places of their own.  Where not, the product before is issued late, behind
-          // the scores of both query tiles, and a store on the way would wait for it in the middle of the exponentials.
+          // the scores of both query tiles, and a store on the way would wait for it in the middle of the exponentials.  24 x 4 680 of 128 channels over 42 120:
+          // after 80 of the 128 keys 2 390 us, 112 2 300, at the end 2 265; 12 sequences of 64 channels with a window: after 64 83.0, 80 80.8, at the end 84.1.
           if (i == (F::kShared ? 7 : 4)) {
             if (t > sg.tb) {                           // the last product has read the weights before
               ok = all_lanes(cx.wait(F::kODone + qt, (n - 1) & 1, 724));
@@ -825,7 +831,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     tc_fence_before();
   } else {
     // ================= expanding warps: values of a tile to FP16 =================
-    setmaxnreg_dec<kRegsExpand>();
+    setmaxnreg_dec<F::kRegsExpand>();
     const int dt = tid - 384;
     Reader<D> w(cx, smem);
     Segment sg;
