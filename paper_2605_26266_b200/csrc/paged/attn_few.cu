@@ -162,11 +162,6 @@ __device__ __forceinline__ bool barrier_or(uint32_t id, uint32_t n, bool x) {
                : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)x) : "memory");
   return r != 0;
 }
-// 16 bytes from global to shared memory, on their way until copies_done().
-__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r) {
 #pragma unroll
