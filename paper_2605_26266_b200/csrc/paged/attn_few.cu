@@ -162,6 +162,27 @@ __device__ __forceinline__ bool barrier_or(uint32_t id, uint32_t n, bool x) {
                : "=r"(r) : "r"(id), "r"(n), "r"((uint32_t)x) : "memory");
   return r != 0;
 }
+// Sums over the warp of each of N numbers: the result is the lane's row, whose sum is in x[0]; 32 / N neighbouring lanes have the same one.
+template <int N>
+__device__ __forceinline__ int sum_rows(float (&x)[N]) {
+  const int lane = threadIdx.x & 31;
+  int row = 0;
+#pragma unroll
+  for (int half = N / 2, mask = 16; mask; half >>= 1, mask >>= 1) {
+    if (half) {                                                     // one half of the rows goes to the other lane, whose part of the other half comes here
+      const bool upper = lane & mask;
+      row += upper ? half : 0;
+#pragma unroll
+      for (int i = 0; i < half; ++i) {
+        const float send = upper ? x[i] : x[i + half], keep = upper ? x[i + half] : x[i];
+        x[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, send, mask);
+      }
+    } else {
+      x[0] += __shfl_xor_sync(0xFFFFFFFFu, x[0], mask);
+    }
+  }
+  return row;
+}
 template <int N>
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r) {
 #pragma unroll
@@ -550,35 +571,10 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       const bool any = mine >= it0 - tiles, two = tiles > 1 || (it0 - 1 & 1);      // the second group has one
       if (any) ok = ok && __all_sync(0xFFFFFFFFu, cx.wait(F::kPDone + grp, mine >> 1 & 1, 625));
       if (barrier_or(3, 256, !ok)) { ok = false; break; }
-      // over the buffers of the weights, whose last products are done
-      float* sums = reinterpret_cast<float*>(smem + F::kOffP);
-      auto factor = [&](int r) { return ex2(fminf(shifts[r], shifts[NR + r]) - shift[r]); };      // to the maximum of both groups
-      if (two) {
-        if (grp == 1) {
-#pragma unroll
-          for (int r = 0; r < NR; ++r) sums[r * 128 + key] = l[r] * factor(r);
-        }
-        named_barrier_sync(3, 256);
-        if (grp == 0) {
-#pragma unroll
-          for (int r = 0; r < NR; ++r) l[r] = fmaf(l[r], factor(r), sums[r * 128 + key]);
-        }
-      }
-      if (grp == 0) {
-        constexpr int kPer = 128 / NR;                              // threads of a row
-#pragma unroll
-        for (int r = 0; r < NR; ++r) sums[r * 128 + key] = l[r];
-        named_barrier_sync(1, 128);
-        const float4* from = reinterpret_cast<const float4*>(sums + key / kPer * 128) + key % kPer;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < NR / 4; ++i) {
-          const float4 x = from[i * kPer];
-          sum += (x.x + x.y) + (x.z + x.w);
-        }
-#pragma unroll
-        for (int i = kPer / 2; i; i >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, i);
-        if (key % kPer == 0) { part[key / kPer] = sum; drop[key / kPer] = sum == 0.f ? 0.f : 1.f / sum; }
+      auto factor = [&](int g, int r) { return ex2(fminf(shifts[r], shifts[NR + r]) - shifts[g * NR + r]); };      // to the maximum of both groups
+      {
+        const int row = sum_rows<NR>(l);                            // l[0] is that row's now, of the warp's keys
+        if (lane % (32 / NR) == 0) part[wq * NR + row] = l[0];
       }
       float o[NR];
 #pragma unroll
@@ -590,27 +586,34 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         tmem_wait_ld();
         tc_fence_before();
 #pragma unroll
-        for (int r = 0; r < NR; ++r) o[r] = fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r]));
+        for (int r = 0; r < NR; ++r) o[r] = fmaf(__uint_as_float(raw[NR + r]), 0x1p-4f, __uint_as_float(raw[r])) * factor(grp, r);
       }
-      if (two) {
-        named_barrier_sync(3, 256);                                 // sums are read
-        if (grp == 1) {
+      // over the buffers of the weights, whose last products are done
+      float* sums = reinterpret_cast<float*>(smem + F::kOffP);
+      if (grp == 1 && two) {
 #pragma unroll
-          for (int r = 0; r < NR; ++r) sums[r * 128 + key] = o[r] * factor(r);
-        }
-        named_barrier_sync(3, 256);
-        if (grp == 0) {
-#pragma unroll
-          for (int r = 0; r < NR; ++r) o[r] = fmaf(o[r], factor(r), sums[r * 128 + key]);
-        }
+        for (int r = 0; r < NR; ++r) sums[r * 128 + key] = o[r];
       }
+      named_barrier_sync(3, 256);
       if (grp == 1) {
         named_barrier_sync(3, 256);                                 // buffers and maxima are the next segment's now
         ++nseg;
         continue;
       }
-      named_barrier_sync(1, 128);                                   // sums of the rows; nobody needs the maxima apart any more
-      if (key < NR) shift[key] = fminf(shifts[key], shifts[NR + key]);
+      if (two) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) o[r] += sums[r * 128 + key];
+      }
+      if (key < NR) {
+        const float* other = part + 4 * NR;
+        const float a = (part[key] + part[NR + key]) + (part[2 * NR + key] + part[3 * NR + key]);
+        const float b = (other[key] + other[NR + key]) + (other[2 * NR + key] + other[3 * NR + key]);
+        const float sum = fmaf(a, factor(0, key), b * factor(1, key));
+        part[key] = sum;
+        drop[key] = sum == 0.f ? 0.f : 1.f / sum;
+        shift[key] = fminf(shifts[key], shifts[NR + key]);
+      }
+      named_barrier_sync(1, 128);
       const bool whole = sg.tb == 0 && sg.te == sg.n;
       const int slot = nseg == 0 ? 0 : 1;
       float* to = whole ? nullptr : reinterpret_cast<float*>(p.slots + (size_t)(2 * blockIdx.x + slot) * F::kSlotBytes);
