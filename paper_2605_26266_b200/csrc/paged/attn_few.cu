@@ -14,8 +14,8 @@
 // Work: the tiles (128 tokens) of all (sequence, key head) units in one line, cut evenly over the CTAs; lengths are on the device, so every CTA finds
 // its place in the line itself.  Units that are cut leave FP32 partial rows for the merge kernel.
 //
-// 64 requests of up to 16 384 tokens, 32 query heads on 8 of 128 channels: 199 to 209 us, 5.7 to 5.9 TB/s of codes; one request of 149 760: 61 us, 5.0 TB/s, the
-// rest its start, the last tile's chain and the merge; 16 tokens of 32 heads over 16 384: 38 us, 3.6 TB/s, of which 25 are the bytes'.
+// 64 requests of up to 16 384 tokens, 32 query heads on 8 of 128 channels: 196 to 202 us, 5.9 to 6.0 TB/s of codes; one request of 149 760: 61 us, 5.0 TB/s, the
+// rest its start, the last tile's chain and the merge; 16 tokens of 32 heads over 16 384: 35.5 us, 3.8 TB/s, of which 25 are the bytes'.
 #include "tensor.cuh"
 
 namespace kvq {
@@ -718,9 +718,9 @@ int launch(const AttnCall& c, const CUtensorMap& mk, const CUtensorMap& mv, cons
 }
 
 // A CTA for each unit and no merge, where there are no more units than SMs and their sequences are short (by the width of the table's rows, all that the host
-// knows of them).  Whole against cut, us from a graph: 2 units of 64 channels of 4 tiles 6.9 / 8.3, of 6 8.1 / 8.9, of 8 9.6 / 8.3; 128 units of 6 tiles
-// 10.1 / 14.6 (128 channels), of 12 14.3 / 18.3; 256 units of one tile 11.1 / 10.1.
-constexpr int kWholeTiles = 6, kWholeTilesMany = 12;
+// knows of them).  Whole against cut, us from a graph: 2 units of 64 channels of 4 tiles 7.2 / 8.9, of 6 9.0 / 9.9, of 8 10.7 / 9.2; 8 units of 16 rows, 128 channels,
+// of 6 tiles 11.1 / 13.0, of 8 12.7 / 12.3; 128 units of 128 channels of 12 tiles 12.8 / 17.5, of 24 22.0 / 24.1.
+constexpr int kWholeTiles = 6, kWholeTilesMany = 24;
 bool take_whole(const AttnCall& c, int sms) {
   const int64_t units = (int64_t)c.seqs.batch * c.pool.kv_heads, tokens = (int64_t)c.seqs.width * c.pool.page;
   return units <= sms && tokens <= (2 * units > sms ? kWholeTilesMany : kWholeTiles) * kTileKeys;
