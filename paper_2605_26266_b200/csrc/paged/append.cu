@@ -431,10 +431,12 @@ __global__ void __launch_bounds__(run_threads_of(D, PAGE), 512 / run_threads_of(
   if (far) report(p.status, kBadPosition);
 }
 
-// Runs, where blocks are at least five times as many as run at a time: fewer do not pay for a run's start and leave CTAs with a block more than others.  A CTA
-// each against runs, us from a graph, one sequence, 8 heads, blocks 2, 4, 6 and 10 times as many as run at a time: 128 channels, pages of 128 6.6 / 9.7, 11.8 / 14.8,
-// 20.7 / 20.0, 38.5 / 32.0; 64 channels, pages of 16 7.6 / 7.8, 12.8 / 12.1, 19.0 / 17.4, 32.2 / 30.4.
-constexpr int kRunRounds = 5;
+// Runs, where blocks are at least five times as many as run at a time and sequences have new tokens for several pages; of fewer the start of a run and the place in
+// the line are not paid for.  A CTA each against runs, us from a graph.  One sequence, 8 heads, blocks 2, 4, 6 and 10 times as many as run at a time: 128
+// channels, pages of 128 6.6 / 9.7, 11.8 / 14.8, 20.7 / 20.0, 38.5 / 32.0; 64 channels, pages of 16 7.6 / 7.8, 12.8 / 12.1, 19.0 / 17.4, 32.2 / 30.4.  128
+// sequences, 128 channels, pages of 64, each with new tokens of 2, 4 and 8 pages 26.5 / 25.2, 49.6 / 44.0, 89.0 / 75.0; of up to 2, 4 and 8 pages, which has to be
+// looked up, 15.5 / 21.0, 28.3 / 30.2, 51.8 / 47.4.  2 048 sequences with a token each 55 / 64 and 56 / 107.
+constexpr int kRunRounds = 5, kRunPages = 4, kRunPagesLookedUp = 8;
 template <int D, int PAGE>
 int launch(const AppendCall& c, const AppendParams& p) {
   AppendParams q = p;
@@ -443,7 +445,7 @@ int launch(const AppendCall& c, const AppendParams& p) {
   if (r != KVQ_OK || (r = current_device(&dev)) != KVQ_OK) return r;
   static PerDevice set[2][2];
   const int64_t total = (int64_t)q.blocks * c.pool.kv_heads * c.seqs.batch, at_a_time = (int64_t)sms * (512 / run_threads_of(D, PAGE));
-  const bool runs = total >= kRunRounds * at_a_time;
+  const bool runs = total >= kRunRounds * at_a_time && c.n_tokens >= (c.seqs.n_new ? kRunPagesLookedUp : kRunPages) * PAGE;
   const auto kernel = runs ? p.rope.interleaved ? paged_append_run_kernel<D, PAGE, true> : paged_append_run_kernel<D, PAGE, false>
                            : p.rope.interleaved ? paged_append_kernel<D, PAGE, true> : paged_append_kernel<D, PAGE, false>;
   // the rotated keys, and of a run the rows of two blocks

@@ -57,8 +57,9 @@ def test_runs_are_what_single_blocks_are(B, d, page, ragged, interleaved):
     assert int(status) == 0
 
 
-def test_runs_against_the_definition(B):
-    cache, table, k, v, rope = _inputs(B, 128, 128, NEWS, seed=3)
+@pytest.mark.parametrize("page", [64, 128])
+def test_runs_against_the_definition(B, page):
+    cache, table, k, v, rope = _inputs(B, 128, page, NEWS, seed=3)
     ref = P.Reference(cache)
     B.kvq_paged_append(cache, k, v, table, P.ints(LENS), n_new=P.ints(NEWS), **rope)
     ref.append(k, v, table, P.ints(LENS), P.ints(NEWS), **rope)
